@@ -436,6 +436,214 @@ mot_status mot_backbone_translate(const void* src_k, const void* src_v, const in
                                   const void* params, const mot_router_weights* router, void* dst_k, void* dst_v,
                                   const mot_shapes* shapes, const mot_backbone_dims* dims, hipStream_t stream);
 
+/*
+ * The paged cache: where the target model goes on from its translated context.
+ * A layer's keys and values lie in pools of pages of page_size positions; a
+ * row of the page table names the pages of a sequence in order, so sequences
+ * of different lengths share a pool, grow by a page at a time and share the
+ * pages of a common prefix.
+ *
+ *   k_pages, v_pages  device, dtype: [L][n_pages] x [page_size][H_kv][D]
+ *                (page_layout MOT_LAYOUT_BTHD) or [H_kv][page_size][D] (BHTD)
+ *   table        device int32 [B][max_pages]: entry j of row b is the page
+ *                of positions j * page_size .. + page_size - 1 of sequence b.
+ *                An entry outside 0 .. n_pages - 1 (-1, say) is a hole: its
+ *                positions are neither read nor written
+ *   kv_len       device int32 [B]: positions of each sequence, the new tokens
+ *                of the call among them (cut to 0 .. max_pages * page_size)
+ *   new_start    device int32 [B + 1] or NULL: the new tokens of sequence b
+ *                are the rows new_start[b] .. new_start[b + 1] - 1 of the
+ *                call's row tensors (cut to 0 .. n_new).  NULL: every sequence
+ *                has max_new of them, at batch row b
+ *
+ * New token i of the c of sequence b is at position kv_len[b] - c + i.  Rows
+ * of no sequence are left as they are, and so are, of a sequence with more
+ * than max_new new tokens, those from the max_new-th on.
+ *
+ *   L            layers of the pools (1..MOT_MAX_LAYERS)
+ *   n_pages      pages of a layer's pool
+ *   page_size    positions per page: a power of two, 16 .. 1024
+ *   H_kv, D      KV heads and head dim
+ *   B, max_pages rows and entries per row of the table (max_pages * page_size
+ *                at most 2^30, B at most 65535)
+ *   dtype        MOT_F32 or MOT_BF16
+ *   page_layout  MOT_LAYOUT_BTHD or MOT_LAYOUT_BHTD, see above
+ * A page of a layer is under 2 GiB.
+ */
+typedef struct {
+    int32_t L, n_pages, page_size;
+    int32_t H_kv, D;
+    int32_t B, max_pages;
+    int32_t dtype, page_layout;
+} mot_cache_shapes;
+
+/* Elements from one layer, batch row, token and head of a row tensor to the
+ * next; a head's D elements are contiguous.  With new_start the tokens of all
+ * sequences are in one axis and `batch` is not used.  Multiples of 8 (bf16)
+ * or 4 (fp32), not negative; the rows of an output share no element. */
+typedef struct {
+    int64_t layer, batch, token, head;
+} mot_strides;
+
+/*
+ * Attention of new tokens over the paged cache of one layer (L = 1; pass the
+ * layer's pools): for the new token at position u of sequence b and query
+ * head h, which reads KV head h / (H_q / H_kv),
+ *     o = sum_{v in N} softmax_v(scale q . k[v]) v[v]
+ *     N = { 0 <= v <= u, v > u - window (when window > 0), v in no hole }
+ * and zeros where N is empty.  One new token per sequence is a decoding step,
+ * many are a chunk of a prompt over what is already cached.  Softmax and
+ * accumulation in fp32, o rounded once to dtype (the probabilities of MOT_BF16
+ * are rounded to bf16 for the second product, as replay attention does).
+ * Positions from kv_len on and holes are not looked at, whatever they hold;
+ * a NaN or infinite value reaches the tokens that see it and no others.
+ *
+ *   q, o         device, dtype: rows of the new tokens, strides below (head
+ *                pitch and all); o must not overlap q, the pools or the tables
+ *   n_new        rows of q and o over all sequences (B * max_new without
+ *                new_start)
+ *   max_new      most new tokens of a sequence
+ *   H_q          query heads, a multiple of H_kv
+ *   window       0: every position up to u; else that many, u among them
+ *   max_kv       0, or a bound on kv_len that is better than max_pages *
+ *                page_size (a hint for how work is cut; longer sequences are
+ *                still attended in full)
+ *   scale        0: 1 / sqrt(D); positive
+ *   q, o strides of q and o (layer not used)
+ *   workspace, workspace_bytes
+ *                optional device scratch of this call (16-byte aligned, not
+ *                overlapping its arrays; calls that overlap in time need their
+ *                own).  With at least mot_attend_workspace_bytes, and those not
+ *                0, long sequences are cut along their positions over several
+ *                workgroups, whose partial sums a second kernel joins in a
+ *                fixed order; with less, or NULL, no sequence is cut (same
+ *                results up to the order of fp32 sums)
+ * D is 64 or 128 (else MOT_ERR_UNSUPPORTED).  n_new = 0 and B = 0 are no-ops.
+ * No allocation, no synchronisation; can be captured into a graph.
+ */
+typedef struct {
+    int32_t n_new, max_new;
+    int32_t H_q;
+    int32_t window;
+    int32_t max_kv;
+    float scale;
+    mot_strides q, o;
+    void* workspace;
+    size_t workspace_bytes;
+} mot_attend_shapes;
+
+mot_status mot_paged_attention(const void* q, const void* k_pages, const void* v_pages, const int32_t* table,
+                               const int32_t* kv_len, const int32_t* new_start, void* o,
+                               const mot_cache_shapes* cache, const mot_attend_shapes* shapes, hipStream_t stream);
+
+/* Scratch bytes with which mot_paged_attention cuts calls of these shapes
+ * (0: it would not); SIZE_MAX for invalid or unsupported shapes.  Does not go
+ * by any data. */
+size_t mot_attend_workspace_bytes(const mot_cache_shapes* cache, const mot_attend_shapes* shapes);
+
+/*
+ * New tokens into the paged cache, in one pass over q, k and v: for every new
+ * token and layer l
+ *     x' = gain x / sqrt(mean_d x_d^2 + eps)      (queries with q_gain, keys
+ *                                                  with k_gain, where given)
+ *     each pair (x'_i, x'_j) turned by the angle position * inv_freq[r]
+ *     q_out = queries,  key and value -> the token's place in its page
+ * Pair r of the first rotary_dim elements is (r, r + rotary_dim / 2), or
+ * (2 r, 2 r + 1) when interleaved; the others stay.  Norms, angles and turns
+ * are computed in fp32 (angles in fp64 until they are reduced to one turn) and
+ * rounded once; values are copied.  A token at a negative position or in a
+ * hole is not stored; its query is written all the same.
+ * Without norms and rotation the call stores a translated cache (all layers
+ * at once) into pages.  Tokens of one call must not share a place: a page in
+ * which several rows grow is made several by mot_cache_reorder first.
+ *
+ *   q, q_out     device or NULL (both): [L] rows of H_q heads; q_out may be q
+ *                (same strides), else it must not overlap q, k or v
+ *   k, v         device or NULL (both): [L] rows of H_kv heads
+ *   rope         NULL, or the arrays of
+ *     q_gain, k_gain  device, dtype [L][D], or NULL: no norm
+ *     inv_freq        device float [rotary_dim / 2] or NULL: no rotation
+ *     positions       device int32 [n_new] (packed, or [B][max_new]) or NULL:
+ *                     the position each row is turned by, where it is not the
+ *                     position of its place
+ *   H_q          query heads (not used without q)
+ *   rotary_dim   a multiple of 16, at most D (0: D)
+ *   eps          >= 0
+ * D is a multiple of 16 up to 256.  Same error discipline as mot_translate.
+ */
+typedef struct {
+    const void* q_gain;
+    const void* k_gain;
+    const float* inv_freq;
+    const int32_t* positions;
+} mot_rope;
+
+typedef struct {
+    int32_t n_new, max_new;
+    int32_t H_q;
+    int32_t rotary_dim, interleaved;
+    float eps;
+    mot_strides q, q_out, k, v;
+} mot_append_shapes;
+
+mot_status mot_cache_append(const void* q, const void* k, const void* v, void* q_out, void* k_pages, void* v_pages,
+                            const int32_t* table, const int32_t* kv_len, const int32_t* new_start,
+                            const mot_rope* rope, const mot_cache_shapes* cache, const mot_append_shapes* shapes,
+                            hipStream_t stream);
+
+/*
+ * The next table of the sequences, made from the present one: forking,
+ * copying, cutting back, freeing and growing, for every row at once.  New row
+ * b (of n_rows) takes the first keep[b] positions of row source[b] and has
+ * room for want[b]:
+ *   - pages that the kept positions fill are shared with every other new row
+ *     that keeps them;
+ *   - a last page that they fill in part stays with the lowest row that keeps
+ *     it, unless some row keeps it whole.  The others get a page of their own
+ *     with a copy of the kept positions, in every layer's keys and values;
+ *   - want[b] beyond that is met with pages of unspecified content.
+ * New pages are the lowest-numbered ones that no new row takes over, given out
+ * in the order of rows and of positions within a row; all other pages are
+ * free: a page is in use when the table names it, nothing else is kept.
+ *
+ *   table        device int32 [B][max_pages], read
+ *   source       device int32 [n_rows]; outside 0 .. B - 1: an empty row
+ *   keep, want   device int32 [n_rows], cut to 0 .. max_pages * page_size;
+ *                want below keep means keep.  keep is at most what the source
+ *                row holds; holes among the kept pages stay holes
+ *   new_table    device int32 [n_rows][max_pages], written whole (-1 past the
+ *                pages of a row); not overlapping any other array
+ *   missing      device int32 [1]: pages that could not be had (their entries
+ *                are holes); 0 when the pool sufficed
+ *   workspace    device scratch of this call, at least mot_cache_workspace_bytes
+ *                (16-byte aligned, not overlapping its arrays; calls that
+ *                overlap in time need their own)
+ * Beam search sets source to the parents and want = keep + 1; a beam that ends
+ * has source -1.  n_rows at most 4096 (0: a no-op that writes nothing).  The
+ * data of pages that new rows take over does not move.
+ */
+mot_status mot_cache_reorder(void* k_pages, void* v_pages, const int32_t* table, const int32_t* source,
+                             const int32_t* keep, const int32_t* want, int32_t* new_table, int32_t* missing,
+                             const mot_cache_shapes* cache, int32_t n_rows, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
+/*
+ * The pages in use (those that the table names) moved together to the lowest
+ * numbers, in every layer: with n of them, those numbered n and up go to the
+ * free pages under n, the lowest to the lowest.  new_table: the table with the
+ * new numbers (holes -1), not overlapping any other array; used: device int32
+ * [1], n.  The pool can then be cut to its first n pages.  Moved pages keep
+ * their old content too.  workspace as for mot_cache_reorder.  B = 0 is a no-op
+ * that writes nothing.
+ */
+mot_status mot_cache_compact(void* k_pages, void* v_pages, const int32_t* table, int32_t* new_table, int32_t* used,
+                             const mot_cache_shapes* cache, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
+/* Scratch bytes of mot_cache_reorder for n_rows new rows (n_rows 0: of
+ * mot_cache_compact); SIZE_MAX for invalid shapes. */
+size_t mot_cache_workspace_bytes(const mot_cache_shapes* cache, int32_t n_rows);
+
 /* MOT_ABI_VERSION of the loaded library. */
 int mot_abi_version(void);
 

@@ -12,7 +12,8 @@ def __getattr__(name):
     # lazy: the binding loads libmot.so on first use
     if name in ("translate", "translate_raw", "depth_ratio_map", "workspace_bytes",
                 "abi_version", "status_string", "Shapes", "MotError", "lib_path",
-                "load_library", "MOT_F32", "MOT_BF16"):
+                "load_library", "MOT_F32", "MOT_BF16", "paged_attention", "cache_append", "cache_reorder",
+                "cache_compact"):
         from . import binding
         return getattr(binding, name)
     raise AttributeError(name)

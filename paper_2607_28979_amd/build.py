@@ -22,7 +22,8 @@ LIB = os.path.join(CSRC, "libmot.so")
 # instantiation file is compiled once per (d_in, d_out) so they build in parallel
 SOURCES = [(f, os.path.splitext(f)[0], {}) for f in
            ("mot_api.hip", "k_router.hip", "k_routed.hip", "k_f32.hip", "k_f32_split.hip", "k_bf16_unfused.hip", "k_bf16_gemm256.hip",
-            "k_bf16_fused.hip", "k_project.hip", "k_replay.hip", "k_backbone.hip")]
+            "k_bf16_fused.hip", "k_project.hip", "k_replay.hip", "k_backbone.hip", "cache_api.hip", "k_cache.hip",
+            "k_paged_attn.hip")]
 SOURCES += [("k_bf16_fused_inst.hip", "k_bf16_fused_%d_%d" % (a, b),
              {"MOT_FUSED_D_IN": a, "MOT_FUSED_D_OUT": b})
             for a in (128, 256, 512) for b in (128, 256, 512)]
@@ -31,7 +32,7 @@ SOURCES += [("k_bf16_fused_inst.hip", "k_bf16_fused_%d_%d" % (a, b),
 # GEMM epilogues read them; the AGPR form copies them in and out)
 _VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 EXTRA = {f: _VGPR_FORM for f in ("k_replay.hip", "k_backbone.hip", "k_project.hip", "k_bf16_unfused.hip",
-                            "k_f32_split.hip")}
+                            "k_f32_split.hip", "k_paged_attn.hip")}
 
 
 def hipcc() -> str:

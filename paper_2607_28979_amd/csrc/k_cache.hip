@@ -1,0 +1,473 @@
+// The paged cache: new tokens into their pages (norms and rotation on the
+// way), reordering of the table's rows, compaction of the pool.
+#include "cache_internal.h"
+#include "mot_device.h"
+
+namespace mot {
+
+namespace {
+
+// 8 elements of a row as floats, and back
+__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = bf16_lo(w[i]);
+        x[2 * i + 1] = bf16_hi(w[i]);
+    }
+}
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const f32x4 w = reinterpret_cast<const f32x4*>(p)[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[4 * i + j] = w[j];
+    }
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
+    *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                         pack_bf16x2(x[6], x[7])};
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) reinterpret_cast<f32x4*>(p)[i] = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+}
+
+constexpr int kMostTokens = 4;   // tokens of a workgroup
+
+// Norms, rotation and stores of `tpb` new tokens of one sequence and layer: rows are
+// the token's query, key and value heads, LPR lanes each, two 16-byte chunks of
+// 8 elements (bf16) per lane: c and c + rot / 16 of the rotated part, so that
+// both elements of a half-split pair are in one lane.  Angles are shared by a
+// token's heads: computed once per workgroup, into LDS; position * inv_freq in
+// fp64, since fp32 leaves an error of 2e-3 turns at position 32768.
+//
+// grid (ceil(max_new / tpb), B, L), 256 threads
+template <typename T, int LPR>
+__global__ __launch_bounds__(256) void k_cache_append(AppendProblem p, int tpb) {
+    __shared__ float2 s_turn[kMostTokens][128];
+    __shared__ int64_t s_slot[kMostTokens];   // element offset of the token's place, -1: not stored
+    const int b = blockIdx.y, l = blockIdx.z, tid = threadIdx.x, D = p.c.D;
+    const NewTokens nt = new_tokens(p.c, b);
+    const int i0 = blockIdx.x * tpb, m = min(tpb, nt.n - i0);
+    if (m <= 0) return;   // uniform over the workgroup
+    const int pos0 = nt.kv - nt.count + i0;
+    if (tid < m) {
+        const int pos = pos0 + tid;
+        int64_t at = -1;
+        if (pos >= 0) {
+            const int page = p.c.table[(int64_t)b * p.c.max_pages + (pos >> p.c.page_shift)];
+            if (page >= 0 && page < p.c.n_pages)
+                at = ((int64_t)l * p.c.n_pages + page) * p.c.page_elems +
+                     (int64_t)(pos & ((1 << p.c.page_shift) - 1)) * p.c.ts;
+        }
+        s_slot[tid] = at;
+    }
+    const int half = p.rot >> 1;
+    if (p.inv_freq)
+        for (int x = tid; x < m * half; x += 256) {
+            const int t = x / half, r = x - t * half;
+            const int pos = p.positions ? p.positions[p.c.start ? nt.row + i0 + t : b * p.c.max_new + i0 + t] : pos0 + t;
+            double turns = (double)pos * (double)p.inv_freq[r] * 0.15915494309189533577;
+            turns -= rint(turns);
+            float sn, cs;
+            sincospif(2.0f * (float)turns, &sn, &cs);
+            s_turn[t][r] = make_float2(cs, sn);
+        }
+    __syncthreads();
+    const int nq = p.q ? p.H_q : 0, nk = p.k ? p.c.H_kv : 0, heads = nq + 2 * nk;
+    const int c = tid % LPR, rc = p.rot >> 4, lanes = D >> 4;
+    const bool live = c < lanes, turned = c < rc;
+    const int lo = turned ? c : rc + c, hi = turned ? c + rc : lo + lanes - rc;   // chunks of 8
+    for (int r = tid / LPR; r < m * heads; r += 256 / LPR) {
+        const int t = r / heads, h = r - t * heads;
+        const int kind = h < nq ? 0 : h < nq + nk ? 1 : 2, hh = kind == 0 ? h : kind == 1 ? h - nq : h - nq - nk;
+        const RowStrides& st = kind == 0 ? p.qs : kind == 1 ? p.ks : p.vs;
+        const T* src = reinterpret_cast<const T*>(kind == 0 ? p.q : kind == 1 ? p.k : p.v) + l * st.layer +
+                       row_offset(p.c, st, nt, b, i0 + t) + hh * st.head;
+        T* dst;
+        if (kind == 0) {
+            dst = reinterpret_cast<T*>(p.q_out) + l * p.qos.layer + row_offset(p.c, p.qos, nt, b, i0 + t) + hh * p.qos.head;
+        } else {
+            const int64_t at = s_slot[t];
+            if (at < 0) continue;   // uniform over the row's lanes
+            dst = reinterpret_cast<T*>(kind == 1 ? p.k_pages : p.v_pages) + at + (int64_t)hh * p.c.hs;
+        }
+        float x[8], y[8];
+        if (live) {
+            load8(src + 8 * lo, x);
+            load8(src + 8 * hi, y);
+        }
+        const T* gain = reinterpret_cast<const T*>(kind == 0 ? p.q_gain : kind == 1 ? p.k_gain : nullptr);
+        if (gain) {
+            float ss = 0.f;
+            if (live) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) ss += x[j] * x[j] + y[j] * y[j];
+            }
+#pragma unroll
+            for (int w = 1; w < LPR; w <<= 1) ss += __shfl_xor(ss, w, 64);
+            const float inv = 1.0f / sqrtf(ss / (float)D + p.eps);
+            if (live) {
+                float gx[8], gy[8];
+                load8(gain + (int64_t)l * D + 8 * lo, gx);
+                load8(gain + (int64_t)l * D + 8 * hi, gy);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    x[j] *= inv * gx[j];
+                    y[j] *= inv * gy[j];
+                }
+            }
+        }
+        if (p.inv_freq && kind != 2 && turned) {
+            if (p.interleaved) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 u = s_turn[t][4 * lo + j], v = s_turn[t][4 * hi + j];
+                    const float x0 = x[2 * j], y0 = y[2 * j];
+                    x[2 * j] = x0 * u.x - x[2 * j + 1] * u.y;
+                    x[2 * j + 1] = x[2 * j + 1] * u.x + x0 * u.y;
+                    y[2 * j] = y0 * v.x - y[2 * j + 1] * v.y;
+                    y[2 * j + 1] = y[2 * j + 1] * v.x + y0 * v.y;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float2 u = s_turn[t][8 * lo + j];
+                    const float x0 = x[j];
+                    x[j] = x0 * u.x - y[j] * u.y;
+                    y[j] = y[j] * u.x + x0 * u.y;
+                }
+            }
+        }
+        if (live) {
+            store8(dst + 8 * lo, x);
+            store8(dst + 8 * hi, y);
+        }
+    }
+}
+
+template <typename T>
+hipError_t append_as(const AppendProblem& p, hipStream_t stream) {
+    // one token per workgroup until there are several for every CU
+    const int64_t tokens = (int64_t)p.c.max_new * p.c.B * p.L;
+    const int tpb = tokens >= 2048 ? kMostTokens : 1;
+    const dim3 grid((p.c.max_new + tpb - 1) / tpb, p.c.B, p.L);
+    const int lanes = p.c.D >> 4;
+    if (lanes <= 2) k_cache_append<T, 2><<<grid, 256, 0, stream>>>(p, tpb);
+    else if (lanes <= 4) k_cache_append<T, 4><<<grid, 256, 0, stream>>>(p, tpb);
+    else if (lanes <= 8) k_cache_append<T, 8><<<grid, 256, 0, stream>>>(p, tpb);
+    else k_cache_append<T, 16><<<grid, 256, 0, stream>>>(p, tpb);
+    return hipGetLastError();
+}
+
+// ---- pages ----------------------------------------------------------------
+
+constexpr int kThreads = 1024;   // of the one workgroup that gives out pages
+
+// Workspace of reordering and compaction (int32 words), W = words of a bit per
+// page.
+struct PagesWs {
+    uint32_t* held;    // [W] pages that new rows (or the table) name
+    uint32_t* whole;   // [W] reorder: pages that a new row keeps whole
+    int32_t* first;    // [n_pages] reorder: lowest row that keeps the page in part
+    int32_t* list;     // [n_pages] reorder: free pages to give out; compact: targets of moves
+    int32_t* from;     // [n_pages] compact: pages to move
+    int32_t* rank;     // [W + 1] compact: held pages before each word
+    int32_t* base;     // [n_rows] reorder: pages given out before each row
+    int4* pair;        // [n_rows] reorder: (source page, new page, positions) of each copy
+    int32_t* n_pair;   // [1] copies or moves
+};
+size_t r64(size_t n) { return (n + 63) & ~size_t(63); }
+size_t ws_words(int64_t n_pages, int64_t n_rows, const void* at, PagesWs* out) {
+    const size_t W = r64((size_t)(n_pages + 31) / 32 + 1), P = r64((size_t)n_pages), R = r64((size_t)n_rows);
+    int32_t* c = reinterpret_cast<int32_t*>(const_cast<void*>(at));
+    size_t n = 0;
+    auto take = [&](size_t k) { int32_t* r = c + n; n += k; return r; };
+    PagesWs w;
+    w.pair = reinterpret_cast<int4*>(take(4 * R));
+    w.held = reinterpret_cast<uint32_t*>(take(W));
+    w.whole = reinterpret_cast<uint32_t*>(take(n_rows ? W : 0));
+    w.first = take(n_rows ? P : 0);
+    w.list = take(P);
+    w.from = take(n_rows ? 0 : P);
+    w.rank = take(n_rows ? 0 : W);
+    w.base = take(R);
+    w.n_pair = take(64);
+    if (out) *out = w;
+    return n;
+}
+
+// kept, whole and wanted pages of new row b
+struct RowPlan {
+    int32_t src, full, kept, need, rest;   // rest: positions of the last page, in part
+};
+__device__ __forceinline__ RowPlan row_plan(const PagesProblem& p, int b) {
+    RowPlan r;
+    const int sh = p.c.page_shift, most = p.c.max_pages << sh;
+    r.src = p.source[b];
+    const bool ok = r.src >= 0 && r.src < p.c.B;
+    const int keep = ok ? min(max(p.keep[b], 0), most) : 0, want = max(min(p.want[b], most), keep);
+    if (!ok) r.src = 0;
+    r.full = keep >> sh;
+    r.rest = keep - (r.full << sh);
+    r.kept = r.full + (r.rest > 0);
+    r.need = (want + (1 << sh) - 1) >> sh;
+    return r;
+}
+
+__device__ __forceinline__ bool bit_of(const uint32_t* w, int page) { return (w[page >> 5] >> (page & 31)) & 1u; }
+
+__global__ __launch_bounds__(256) void k_pages_clear(PagesProblem p, PagesWs w) {
+    const int W = (p.c.n_pages + 31) / 32, i = blockIdx.x * 256 + threadIdx.x;
+    if (i < W) {
+        w.held[i] = 0;
+        if (p.n_rows) w.whole[i] = 0;
+    }
+    if (p.n_rows && i < p.c.n_pages) w.first[i] = INT32_MAX;
+}
+
+// grid (ceil(max_pages / 256), rows)
+__global__ __launch_bounds__(256) void k_pages_mark(PagesProblem p, PagesWs w) {
+    const int b = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;
+    if (p.n_rows) {
+        const RowPlan r = row_plan(p, b);
+        if (j >= r.kept) return;
+        const int page = p.c.table[(int64_t)r.src * p.c.max_pages + j];
+        if (page < 0 || page >= p.c.n_pages) return;
+        atomicOr(w.held + (page >> 5), 1u << (page & 31));
+        if (j < r.full) atomicOr(w.whole + (page >> 5), 1u << (page & 31));
+        else atomicMin(w.first + page, b);
+    } else {
+        if (j >= p.c.max_pages) return;
+        const int page = p.c.table[(int64_t)b * p.c.max_pages + j];
+        if (page >= 0 && page < p.c.n_pages) atomicOr(w.held + (page >> 5), 1u << (page & 31));
+    }
+}
+
+// Exclusive sum over the workgroup's threads; *all: the total.
+__device__ __forceinline__ int block_scan(int x, int* s_wave, int* all) {
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    int y = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int z = __shfl_up(y, d, 64);
+        if (lane >= d) y += z;
+    }
+    __syncthreads();   // the last call's sums are read
+    if (lane == 63) s_wave[wv] = y;
+    __syncthreads();
+    int before = 0, sum = 0;
+    for (int i = 0; i < kThreads / 64; ++i) {
+        const int n = s_wave[i];
+        before += i < wv ? n : 0;
+        sum += n;
+    }
+    *all = sum;
+    return before + y - x;
+}
+
+// One workgroup: what each row needs, the free pages in order, the copies.
+__global__ __launch_bounds__(kThreads) void k_pages_give(PagesProblem p, PagesWs w) {
+    __shared__ int s_wave[kThreads / 64];
+    const int tid = threadIdx.x, W = (p.c.n_pages + 31) / 32;
+    int asked = 0, copies = 0, all;
+    for (int b0 = 0; b0 < p.n_rows; b0 += kThreads) {
+        const int b = b0 + tid;
+        int need = 0, copy = 0, page = -1, rest = 0;
+        if (b < p.n_rows) {
+            const RowPlan r = row_plan(p, b);
+            if (r.rest) {
+                page = p.c.table[(int64_t)r.src * p.c.max_pages + r.full];
+                copy = page >= 0 && page < p.c.n_pages && (bit_of(w.whole, page) || w.first[page] != b);
+                rest = r.rest;
+            }
+            need = copy + max(r.need - r.kept, 0);
+        }
+        const int at = asked + block_scan(need, s_wave, &all);
+        asked += all;
+        const int c = copies + block_scan(copy, s_wave, &all);
+        copies += all;
+        if (b < p.n_rows) w.base[b] = at;
+        if (copy) w.pair[c] = make_int4(page, at, rest, 0);   // the page's place in the list, for now
+    }
+    int n_free = 0;
+    for (int i0 = 0; i0 < W; i0 += kThreads) {
+        const int i = i0 + tid;
+        uint32_t f = i < W ? ~w.held[i] : 0u;
+        if (i == W - 1 && (p.c.n_pages & 31)) f &= (1u << (p.c.n_pages & 31)) - 1u;
+        int at = n_free + block_scan(__popc(f), s_wave, &all);
+        n_free += all;
+        for (; f && at < asked; f &= f - 1, ++at) w.list[at] = 32 * i + __ffs(f) - 1;
+        if (n_free >= asked) break;   // uniform
+    }
+    __syncthreads();
+    for (int c = tid; c < copies; c += kThreads) {
+        const int at = w.pair[c].y;
+        w.pair[c].y = at < n_free ? w.list[at] : -1;
+    }
+    if (tid == 0) {
+        *w.n_pair = copies;
+        *p.count = max(asked - n_free, 0);
+    }
+    // how many of the list exist, for the rows' tables
+    if (tid == 0) w.n_pair[1] = min(asked, n_free);
+}
+
+// One workgroup: held pages before every word, the moves.
+__global__ __launch_bounds__(kThreads) void k_pages_squeeze(PagesProblem p, PagesWs w) {
+    __shared__ int s_wave[kThreads / 64];
+    const int tid = threadIdx.x, W = (p.c.n_pages + 31) / 32;
+    int used = 0, all;
+    for (int i0 = 0; i0 < W; i0 += kThreads) {
+        const int i = i0 + tid, at = block_scan(i < W ? __popc(w.held[i]) : 0, s_wave, &all);
+        if (i < W) w.rank[i] = used + at;
+        used += all;
+    }
+    __syncthreads();
+    // held pages before page `used`: those that stay
+    const int uw = used >> 5, stay = used == 0 ? 0
+        : uw < W ? w.rank[uw] + __popc(w.held[uw] & ((1u << (used & 31)) - 1u)) : used;
+    for (int i = tid; i < W; i += kThreads) {
+        const uint32_t h = w.held[i];
+        int before = w.rank[i];
+        for (int k = 0; k < 32 && 32 * i + k < p.c.n_pages; ++k) {
+            const int page = 32 * i + k;
+            if ((h >> k) & 1u) {
+                if (page >= used) w.from[before - stay] = page;
+                ++before;
+            } else if (page < used) {
+                w.list[page - before] = page;
+            }
+        }
+    }
+    if (tid == 0) {
+        *w.n_pair = used - stay;
+        w.n_pair[1] = stay;
+        *p.count = used;
+    }
+}
+
+constexpr int kCopyBytes = 16384;   // of one work item
+
+// The new table (the first `tables` workgroups), and the copies: work items are
+// pieces of kCopyBytes of a page of a layer's keys or values.
+__global__ __launch_bounds__(256) void k_pages_apply(PagesProblem p, PagesWs w, int tables) {
+    const int tid = threadIdx.x, M = p.c.max_pages;
+    if ((int)blockIdx.x < tables) {
+        const int rows = p.n_rows ? p.n_rows : p.c.B;
+        const int64_t at = (int64_t)blockIdx.x * 256 + tid;
+        if (at >= (int64_t)rows * M) return;
+        const int b = (int)(at / M), j = (int)(at - (int64_t)b * M);
+        int page = -1;
+        if (p.n_rows) {
+            const RowPlan r = row_plan(p, b);
+            const int given = w.n_pair[1];
+            int ask = -1;   // place in the list
+            if (j < r.kept) {
+                page = p.c.table[(int64_t)r.src * M + j];
+                if (page < 0 || page >= p.c.n_pages) page = -1;
+            }
+            // a copied last page takes the row's first place in the list, added pages the next
+            int copied = 0;
+            if (r.rest && j >= r.full) {
+                const int last = p.c.table[(int64_t)r.src * M + r.full];
+                copied = last >= 0 && last < p.c.n_pages && (bit_of(w.whole, last) || w.first[last] != b);
+            }
+            if (j == r.full && r.rest && copied) ask = w.base[b];
+            else if (j >= r.kept && j < r.need) ask = w.base[b] + copied + j - r.kept;
+            if (ask >= 0) page = ask < given ? w.list[ask] : -1;
+        } else {
+            page = p.c.table[at];
+            if (page < 0 || page >= p.c.n_pages) page = -1;
+            else if (page >= *p.count)
+                page = w.list[w.rank[page >> 5] + __popc(w.held[page >> 5] & ((1u << (page & 31)) - 1u)) - w.n_pair[1]];
+        }
+        p.new_table[at] = page;
+        return;
+    }
+    const int n = *w.n_pair, sides = 2 * p.L;
+    const int64_t page_bytes = p.c.page_elems * p.elem_bytes;
+    const int pieces = (int)((page_bytes + kCopyBytes - 1) / kCopyBytes);
+    const int64_t items = (int64_t)n * sides * pieces;
+    const int64_t row_bytes = (int64_t)p.c.D * p.elem_bytes;
+    for (int64_t it = blockIdx.x - tables; it < items; it += gridDim.x - tables) {
+        const int piece = (int)(it % pieces), side = (int)(it / pieces % sides), c = (int)(it / pieces / sides);
+        int src, dst;
+        int64_t run = page_bytes;   // contiguous bytes, of each head where the heads come first
+        int runs = 1;
+        int64_t pitch = 0;
+        if (p.n_rows) {
+            const int4 pr = w.pair[c];
+            src = pr.x;
+            dst = pr.y;
+            if (dst < 0) continue;
+            if (p.heads_first) {
+                run = pr.z * row_bytes;
+                runs = p.c.H_kv;
+                pitch = row_bytes << p.c.page_shift;
+            } else {
+                run = pr.z * row_bytes * p.c.H_kv;
+            }
+        } else {
+            src = w.from[c];
+            dst = w.list[c];
+        }
+        char* pool = reinterpret_cast<char*>(side & 1 ? p.v_pages : p.k_pages) + (int64_t)(side >> 1) * p.c.n_pages * page_bytes;
+        const char* from = pool + src * page_bytes;
+        char* to = pool + dst * page_bytes;
+        const int chunks = (int)(run / 16);   // 16-byte chunks of a run
+        const int end = min((piece + 1) * (kCopyBytes / 16), chunks * runs);
+        for (int x = piece * (kCopyBytes / 16) + tid; x < end; x += 256) {
+            const int y = x / chunks;
+            const int64_t off = y * pitch + (int64_t)(x - y * chunks) * 16;
+            *reinterpret_cast<u32x4*>(to + off) = *reinterpret_cast<const u32x4*>(from + off);
+        }
+    }
+}
+
+hipError_t pages_apply(const PagesProblem& p, const PagesWs& w, hipStream_t stream) {
+    const int64_t entries = (int64_t)(p.n_rows ? p.n_rows : p.c.B) * p.c.max_pages;
+    const int tables = (int)((entries + 255) / 256);
+    k_pages_apply<<<tables + 2048, 256, 0, stream>>>(p, w, tables);
+    return hipGetLastError();
+}
+
+hipError_t pages_mark(const PagesProblem& p, const PagesWs& w, hipStream_t stream) {
+    const int W = (p.c.n_pages + 31) / 32, clear = p.n_rows ? p.c.n_pages : W;
+    k_pages_clear<<<(clear + 255) / 256, 256, 0, stream>>>(p, w);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    k_pages_mark<<<dim3((p.c.max_pages + 255) / 256, p.n_rows ? p.n_rows : p.c.B), 256, 0, stream>>>(p, w);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cache_append(const AppendProblem& p, bool bf16, hipStream_t stream) {
+    return bf16 ? append_as<uint16_t>(p, stream) : append_as<float>(p, stream);
+}
+
+size_t pages_workspace_bytes(int64_t n_pages, int64_t n_rows) { return 4 * ws_words(n_pages, n_rows, nullptr, nullptr); }
+
+hipError_t launch_cache_reorder(const PagesProblem& p, hipStream_t stream) {
+    PagesWs w;
+    ws_words(p.c.n_pages, p.n_rows, p.ws, &w);
+    hipError_t e = pages_mark(p, w, stream);
+    if (e != hipSuccess) return e;
+    k_pages_give<<<1, kThreads, 0, stream>>>(p, w);
+    e = hipGetLastError();
+    return e != hipSuccess ? e : pages_apply(p, w, stream);
+}
+
+hipError_t launch_cache_compact(const PagesProblem& p, hipStream_t stream) {
+    PagesWs w;
+    ws_words(p.c.n_pages, 0, p.ws, &w);
+    hipError_t e = pages_mark(p, w, stream);
+    if (e != hipSuccess) return e;
+    k_pages_squeeze<<<1, kThreads, 0, stream>>>(p, w);
+    e = hipGetLastError();
+    return e != hipSuccess ? e : pages_apply(p, w, stream);
+}
+
+}  // namespace mot

@@ -8,15 +8,16 @@
 #include <mutex>
 
 #include "../../include/mot.h"
+#include "api_common.h"
 #include "mot_internal.h"
 
 using namespace mot;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}  // namespace
 
-mot_status fail(mot_status s, const char* fmt, ...) {
+mot_status mot::fail(mot_status s, const char* fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(g_err, sizeof g_err, fmt, ap);
@@ -24,12 +25,14 @@ mot_status fail(mot_status s, const char* fmt, ...) {
     return s;
 }
 
+void mot::clear_error() { g_err[0] = 0; }
+
+namespace {
+
 constexpr size_t kAlign = 256;
 constexpr size_t kDefaultHiddenCap = size_t(1) << 30;   // hidden buffer per group, bytes
 
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 struct Plan {
     bool bf16 = false;
@@ -220,11 +223,6 @@ mot_status owned_workspace(size_t need, void** out) {
     }
     *out = b.ptr;
     return MOT_OK;
-}
-
-bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
-    return na && nb && pa < pb + nb && pb < pa + na;
 }
 
 }  // namespace
