@@ -125,6 +125,8 @@ mot_status check_attend(const mot_cache_shapes* c, const mot_attend_shapes* s, b
     if (st != MOT_OK) return st;
     if (s->H_q < 1 || s->H_q % c->H_kv || (int64_t)s->H_q * c->D > 1 << 20)
         return fail(MOT_ERR_BAD_SHAPE, "H_q=%d: need a positive multiple of H_kv=%d, rows up to 2^20 wide", s->H_q, c->H_kv);
+    if ((int64_t)s->max_new * s->H_q > 1 << 30)
+        return fail(MOT_ERR_BAD_SHAPE, "max_new=%d: more than 2^30 query rows of a sequence", s->max_new);
     if (s->window < 0 || s->max_kv < 0)
         return fail(MOT_ERR_BAD_SHAPE, "window=%d max_kv=%d must be >= 0", s->window, s->max_kv);
     if (!(s->scale >= 0.f) || isinf(s->scale)) return fail(MOT_ERR_BAD_SHAPE, "scale must be positive (0: 1 / sqrt(D))");

@@ -94,6 +94,20 @@ def test_attention_no_ops(lib):
         mb.attend_workspace_bytes(_cache(D=80), s)
 
 
+def test_attention_workspace(lib):
+    # a long decoding step is cut, and its workspace is checked where it is used
+    c = _cache(B=1, max_pages=2048, H_kv=2)
+    s = mb._AttendShapes(1, 1, 4, 0, 0, 0.0, _rows(4, 64, 1), _rows(4, 64, 1))
+    need = mb.attend_workspace_bytes(c, s)
+    assert need > 0 and need % 4 == 0
+    free = FAKE + 40 * GIB
+    kw = dict(cache=c, n_new=1, max_new=1, workspace_bytes=need)
+    assert _attend(workspace=free + 8, **kw) == "MOT_ERR_MISALIGNED"
+    for at, n in ((FAKE, 4 * 64 * 2), (FAKE + GIB, 64 * 16 * 128 * 2), (FAKE + 3 * GIB, 2048 * 4), (FAKE + 5 * GIB, 512)):
+        assert _attend(workspace=at + n - 16, **kw) == "MOT_ERR_BAD_SHAPE"
+        assert _attend(workspace=at - need + 16, **kw) == "MOT_ERR_BAD_SHAPE"
+
+
 def _append(cache=None, ptrs=None, rope=None, strides=None, **kw):
     c = cache or _cache()
     base = dict(n_new=12, max_new=4, H_q=4, rotary_dim=0, interleaved=0, eps=1e-6)
