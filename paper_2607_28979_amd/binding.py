@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
@@ -128,6 +129,7 @@ class Shapes:
 
 
 _lib = None
+_SIZE_MAX = ctypes.c_size_t(-1).value
 
 
 def lib_path() -> str:
@@ -204,19 +206,15 @@ def load_library():
         for fn in (lib.mot_replay_attention, lib.mot_replay_attention_noalloc):
             fn.restype = ctypes.c_int
             fn.argtypes = [ctypes.c_void_p] * 5 + [ctypes.POINTER(_ReplayShapes), ctypes.c_void_p]
-        P, cache = ctypes.c_void_p, ctypes.POINTER(_CacheShapes)
-        lib.mot_paged_attention.restype = ctypes.c_int
-        lib.mot_paged_attention.argtypes = [P] * 7 + [cache, ctypes.POINTER(_AttendShapes), P]
-        lib.mot_attend_workspace_bytes.restype = ctypes.c_size_t
-        lib.mot_attend_workspace_bytes.argtypes = [cache, ctypes.POINTER(_AttendShapes)]
-        lib.mot_cache_append.restype = ctypes.c_int
-        lib.mot_cache_append.argtypes = [P] * 9 + [ctypes.POINTER(_Rope), cache, ctypes.POINTER(_AppendShapes), P]
-        lib.mot_cache_reorder.restype = ctypes.c_int
-        lib.mot_cache_reorder.argtypes = [P] * 8 + [cache, ctypes.c_int32, P, ctypes.c_size_t, P]
-        lib.mot_cache_compact.restype = ctypes.c_int
-        lib.mot_cache_compact.argtypes = [P] * 5 + [cache, P, ctypes.c_size_t, P]
-        lib.mot_cache_workspace_bytes.restype = ctypes.c_size_t
-        lib.mot_cache_workspace_bytes.argtypes = [cache, ctypes.c_int32]
+        P = ctypes.c_void_p
+        for name, res, args in (("mot_paged_attention", ctypes.c_int, [P] * 10),
+                                ("mot_attend_workspace_bytes", ctypes.c_size_t, [P] * 2),
+                                ("mot_cache_append", ctypes.c_int, [P] * 13),
+                                ("mot_cache_reorder", ctypes.c_int, [P] * 9 + [ctypes.c_int32, P, ctypes.c_size_t, P]),
+                                ("mot_cache_compact", ctypes.c_int, [P] * 7 + [ctypes.c_size_t, P]),
+                                ("mot_cache_workspace_bytes", ctypes.c_size_t, [P, ctypes.c_int32])):
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = res, args
         _lib = lib
     return _lib
 
@@ -488,99 +486,123 @@ def backbone_translate(src_k, src_v, layer_map, params, wr, br, dst_k, dst_v, sh
 
 
 # the paged cache --------------------------------------------------------------------------------------------------
+#
+# A decoding step's kernels take a few microseconds, so these calls keep their own
+# share small: sizes go to the library as packed bytes (the layouts of
+# _CacheShapes, _AttendShapes, _AppendShapes and _Rope), checks first, texts only
+# for what fails them.
 
-_TORCH_DTYPE = {}
+_CACHE = struct.Struct("9i")
+_ATTEND = struct.Struct("5if8q")
+_APPEND = struct.Struct("5if16q")
+_ROPE = struct.Struct("4P")
+_SCRATCH = struct.Struct("PN")
+_NO_STRIDES = (0, 0, 0, 0)
+_torch = None
 
 
-def _cache_dtypes():
-    if not _TORCH_DTYPE:
+def _ready():
+    """(the library, torch), loaded."""
+    global _torch
+    if _torch is None:
         import torch
-        _TORCH_DTYPE.update({torch.float32: MOT_F32, torch.bfloat16: MOT_BF16})
-    return _TORCH_DTYPE
+        lib, _torch = load_library(), torch
+    return _lib, _torch
 
 
 def _refuse(status: int, detail: str):
     raise MotError(status, detail)
 
 
-def _pools(k_pages, v_pages, table, page_layout: int) -> _CacheShapes:
+def _stream(dev: int) -> int:
+    return _torch._C._cuda_getCurrentRawStream(dev)
+
+
+class _Pools:
     """The cache's shapes from its tensors: pools [L][n_pages] x page or one
     layer's [n_pages] x page, table int32 [B][max_pages]."""
-    import torch
-    if k_pages.dim() not in (4, 5) or k_pages.shape != v_pages.shape:
-        _refuse(2, "k_pages and v_pages must be alike, [L][n_pages] or [n_pages] x a page of three axes")
-    if k_pages.dtype not in _cache_dtypes() or v_pages.dtype != k_pages.dtype:
-        _refuse(2, "the pools must be float32 or bfloat16 both, not %s, %s" % (k_pages.dtype, v_pages.dtype))
-    if not k_pages.is_contiguous() or not v_pages.is_contiguous():
-        _refuse(2, "the pools must be contiguous")
-    _ints(table, "table", 2, k_pages.get_device())
-    dev = k_pages.get_device()
-    if dev < 0 or dev != torch.cuda.current_device() or v_pages.get_device() != dev:
-        _refuse(1, "the pools are on %s and %s, expected the current device" % (k_pages.device, v_pages.device))
-    *head, a, b, D = k_pages.shape
-    page, heads = (b, a) if page_layout == LAYOUT_BHTD else (a, b)
-    return _CacheShapes(head[0] if len(head) == 2 else 1, head[-1], page, heads, D, table.shape[0], table.shape[1],
-                        _TORCH_DTYPE[k_pages.dtype], page_layout)
+    __slots__ = ("packed", "dtype", "dev", "L", "heads", "D", "B", "max_pages")
+
+    def __init__(self, k_pages, v_pages, table, page_layout: int):
+        torch = _torch
+        shape, dtype, dev = k_pages.shape, k_pages.dtype, k_pages.get_device()
+        n = len(shape)
+        if n not in (4, 5) or shape != v_pages.shape:
+            _refuse(2, "k_pages and v_pages must be alike, [L][n_pages] or [n_pages] x a page of three axes")
+        code = MOT_BF16 if dtype is torch.bfloat16 else MOT_F32
+        if v_pages.dtype is not dtype or (code == MOT_F32 and dtype is not torch.float32):
+            _refuse(2, "the pools must be float32 or bfloat16 both, not %s, %s" % (dtype, v_pages.dtype))
+        if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+            _refuse(2, "the pools must be contiguous")
+        if dev < 0 or v_pages.get_device() != dev or dev != torch._C._cuda_getDevice():
+            _refuse(1, "the pools are on %s and %s, expected the current device" % (k_pages.device, v_pages.device))
+        self.dev, self.dtype = dev, dtype
+        self.ints(table, "table", 2)
+        self.B, self.max_pages = table.shape
+        self.L = shape[0] if n == 5 else 0      # 0: no axis of layers
+        page, self.heads, self.D = shape[-3:]
+        if page_layout == LAYOUT_BHTD:
+            page, self.heads = self.heads, page
+        self.packed = _CACHE.pack(self.L if n == 5 else 1, shape[-4], page, self.heads, self.D, self.B, self.max_pages,
+                                  code, page_layout)
+
+    def ints(self, t, name: str, dims: int, n: Optional[int] = None) -> int:
+        """Address of an int32 tensor."""
+        if t.dtype is not _torch.int32 or t.dim() != dims or not t.is_contiguous() or t.get_device() != self.dev:
+            _refuse(2, "%s must be a contiguous int32 tensor of %d axes on the pools' device" % (name, dims))
+        if n is not None and t.numel() != n:
+            _refuse(2, "%s has %d entries, expected %d" % (name, t.numel(), n))
+        return t.data_ptr()
+
+    def rows(self, t, name: str, lead: tuple, heads: int) -> tuple:
+        """Strides (layer, batch, token, head) of a row tensor [L] x lead x
+        [heads][D] of the pools' type and device."""
+        want = ((self.L,) if self.L else ()) + lead + (heads, self.D)
+        if t.shape != want:
+            _refuse(2, "%s has shape %s, expected %s" % (name, tuple(t.shape), want))
+        if t.dtype is not self.dtype or t.get_device() != self.dev:
+            _refuse(2, "%s is %s on %s, expected the pools' %s on device %d" % (name, t.dtype, t.device, self.dtype, self.dev))
+        st = t.stride()
+        if st[-1] != 1 and self.D > 1:
+            _refuse(2, "%s has a stride of %d between a head's elements" % (name, st[-1]))
+        if 1 in want:       # an axis of one entry may have any stride
+            st = tuple(0 if n == 1 else x for x, n in zip(st, want))
+        return (st[0] if self.L else 0, st[-4] if len(lead) == 2 else 0, st[-3], st[-2])
+
+    def new_rows(self, t, name: str, new_start, max_new) -> tuple:
+        """(leading axes, n_new, max_new) of a call's row tensor."""
+        lead = tuple(t.shape[1 if self.L else 0:-2])
+        axes = "[L]" if self.L else ""
+        if new_start is None:
+            if len(lead) != 2 or lead[0] != self.B:
+                _refuse(2, "%s must be %s[B = %d][new tokens][heads][D] without new_start" % (name, axes, self.B))
+            if max_new is not None and max_new != lead[1]:
+                _refuse(2, "max_new = %d, but %s has %d tokens per sequence" % (max_new, name, lead[1]))
+            return lead, lead[0] * lead[1], lead[1]
+        if len(lead) != 1:
+            _refuse(2, "%s must be %s[new tokens][heads][D] with new_start" % (name, axes))
+        return lead, lead[0], lead[0] if max_new is None else min(int(max_new), lead[0])
+
+    def scratch(self, nbytes: int, given, name: str) -> tuple:
+        """(tensor or None, address, bytes) of a call's scratch: the given one, or
+        torch memory of the current stream."""
+        if given is not None:
+            if given.get_device() != self.dev or not given.is_contiguous():
+                _refuse(2, "%s must be a contiguous tensor on the pools' device" % name)
+            return given, given.data_ptr(), given.numel() * given.element_size()
+        if not nbytes:
+            return None, 0, 0
+        dev = _torch.device("cuda", self.dev)
+        if _captured_outside_torch(dev):
+            return None, 0, 0
+        held = _torch.empty(nbytes, dtype=_torch.uint8, device=dev)
+        return held, held.data_ptr(), nbytes
 
 
-def _ints(t, name: str, dims: int, dev: int, n: Optional[int] = None):
-    import torch
-    if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous() or t.get_device() != dev:
-        _refuse(2, "%s must be a contiguous int32 tensor of %d axes on the pools' device" % (name, dims))
-    if n is not None and t.numel() != n:
-        _refuse(2, "%s has %d entries, expected %d" % (name, t.numel(), n))
-
-
-def _row_strides(t, name: str, like, layers: int, lead: tuple, heads: int, D: int) -> _Strides:
-    """Strides of a row tensor [layers] x lead x [heads][D] (`layers` 0: no such
-    axis) on the pools' device, of their type."""
-    want = ((layers,) if layers else ()) + tuple(lead) + (heads, D)
-    if tuple(t.shape) != want:
-        _refuse(2, "%s has shape %s, expected %s" % (name, tuple(t.shape), want))
-    if t.dtype != like.dtype or t.get_device() != like.get_device():
-        _refuse(2, "%s is %s on %s, expected the pools' %s on %s" % (name, t.dtype, t.device, like.dtype, like.device))
-    st = t.stride()
-    if D > 1 and st[-1] != 1:
-        _refuse(2, "%s has a stride of %d between a head's elements" % (name, st[-1]))
-    # an axis of one entry may have any stride
-    st = [s if n > 1 else 0 for s, n in zip(st, want)]
-    if not layers:
-        st = [0] + st
-    return _Strides(st[0], st[1] if len(lead) == 2 else 0, st[-3], st[-2])
-
-
-def _new_rows(t, name: str, c: _CacheShapes, new_start, max_new, layers: int):
-    """(leading axes, n_new, max_new) of a call's row tensor."""
-    lead = tuple(t.shape[1 if layers else 0:-2])
-    if new_start is None:
-        if len(lead) != 2 or lead[0] != c.B:
-            _refuse(2, "%s must be %s[B = %d][new tokens][heads][D] without new_start" % (name, "[L]" if layers else "", c.B))
-        if max_new is not None and max_new != lead[1]:
-            _refuse(2, "max_new = %d, but %s has %d tokens per sequence" % (max_new, name, lead[1]))
-        return lead, lead[0] * lead[1], lead[1]
-    if len(lead) != 1:
-        _refuse(2, "%s must be %s[new tokens][heads][D] with new_start" % (name, "[L]" if layers else ""))
-    return lead, lead[0], lead[0] if max_new is None else min(int(max_new), lead[0])
-
-
-def _scratch(nbytes: int, dev, given, name: str):
-    """(tensor or None, bytes) of a call's scratch: the given one, or torch memory
-    of the current stream."""
-    import torch
-    if given is not None:
-        if given.get_device() != dev or not given.is_contiguous():
-            _refuse(2, "%s must be a contiguous tensor on the pools' device" % name)
-        return given, given.numel() * given.element_size()
-    if not nbytes or _captured_outside_torch(torch.device("cuda", dev)):
-        return None, 0
-    return torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", dev)), nbytes
-
-
-def attend_workspace_bytes(c: _CacheShapes, s: _AttendShapes) -> int:
-    n = load_library().mot_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(s))
-    if n == ctypes.c_size_t(-1).value:
-        raise MotError(2, load_library().mot_last_error().decode())
-    return int(n)
+def _sized(n: int) -> int:
+    if n == _SIZE_MAX:
+        raise MotError(2, _lib.mot_last_error().decode())
+    return n
 
 
 def paged_attention(q, k_pages, v_pages, table, kv_len, o, new_start=None, max_new: Optional[int] = None,
@@ -598,28 +620,27 @@ def paged_attention(q, k_pages, v_pages, table, kv_len, o, new_start=None, max_n
     ``scratch``: memory for calls that cut long sequences.  None: taken from
     torch's allocator for this call (none under a capture begun outside torch).
     A contiguous tensor: used if it suffices.  False: no cuts."""
-    import torch
-    c = _pools(k_pages, v_pages, table, page_layout)
-    if k_pages.dim() != 4:
+    lib, _ = _ready()
+    c = _Pools(k_pages, v_pages, table, page_layout)
+    if c.L or k_pages.dim() != 4:
         _refuse(2, "attention reads one layer's pools, [n_pages] x page")
-    dev = k_pages.get_device()
-    _ints(kv_len, "kv_len", 1, dev, c.B)
-    if new_start is not None:
-        _ints(new_start, "new_start", 1, dev, c.B + 1)
+    kv = c.ints(kv_len, "kv_len", 1, c.B)
+    start = None if new_start is None else c.ints(new_start, "new_start", 1, c.B + 1)
     if q.dim() < 3:
         _refuse(2, "q must be [B][new][H_q][D] or [tokens][H_q][D]")
-    lead, n_new, mx = _new_rows(q, "q", c, new_start, max_new, 0)
+    lead, n_new, mx = c.new_rows(q, "q", new_start, max_new)
     H_q = q.shape[-2]
     if scale is not None and not scale > 0:
         _refuse(2, "scale must be positive")
-    s = _AttendShapes(n_new, mx, H_q, window, max_kv, scale or 0.0, _row_strides(q, "q", k_pages, 0, lead, H_q, c.D),
-                      _row_strides(o, "o", k_pages, 0, lead, H_q, c.D))
-    lib = load_library()
-    if scratch is None or scratch is not False:
-        held, s.workspace_bytes = _scratch(attend_workspace_bytes(c, s) if scratch is None else 0, dev, scratch, "scratch")
-        s.workspace = _ptr(held)
-    _check(lib.mot_paged_attention(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table), _ptr(kv_len), _ptr(new_start),
-                                   _ptr(o), ctypes.byref(c), ctypes.byref(s), torch.cuda.current_stream().cuda_stream))
+    sizes = _ATTEND.pack(n_new, mx, H_q, window, max_kv, scale or 0.0, *c.rows(q, "q", lead, H_q), *c.rows(o, "o", lead, H_q))
+    held, at, nbytes = None, 0, 0
+    if scratch is not False:
+        need = 0 if scratch is not None else _sized(lib.mot_attend_workspace_bytes(c.packed, sizes + _SCRATCH.pack(0, 0)))
+        held, at, nbytes = c.scratch(need, scratch, "scratch")
+    rc = lib.mot_paged_attention(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), kv, start,
+                                 o.data_ptr(), c.packed, sizes + _SCRATCH.pack(at, nbytes), _stream(c.dev))
+    if rc:
+        _check(rc)
 
 
 def cache_append(q, k, v, q_out, k_pages, v_pages, table, kv_len, new_start=None, max_new: Optional[int] = None,
@@ -633,62 +654,56 @@ def cache_append(q, k, v, q_out, k_pages, v_pages, table, kv_len, new_start=None
     new_start: [tokens][heads][D]), or of L layers [L][n_pages] x page with rows
     [L] x those; any strides with contiguous heads.  q and q_out may be None, or
     the same tensor; k and v may be None."""
-    import torch
-    c = _pools(k_pages, v_pages, table, page_layout)
-    dev, layers = k_pages.get_device(), c.L if k_pages.dim() == 5 else 0
-    _ints(kv_len, "kv_len", 1, dev, c.B)
-    if new_start is not None:
-        _ints(new_start, "new_start", 1, dev, c.B + 1)
+    lib, torch = _ready()
+    c = _Pools(k_pages, v_pages, table, page_layout)
+    kv = c.ints(kv_len, "kv_len", 1, c.B)
+    start = None if new_start is None else c.ints(new_start, "new_start", 1, c.B + 1)
     some = q if k is None else k
     if some is None or (q is None) != (q_out is None) or (k is None) != (v is None):
         _refuse(1, "q with q_out, k with v, and one pair at least")
-    if some.dim() < 3 + (layers > 0):
-        _refuse(2, "rows must be %s[B][new][heads][D] or packed" % ("[L]" if layers else ""))
-    lead, n_new, mx = _new_rows(some, "q" if k is None else "k", c, new_start, max_new, layers)
-    s = _AppendShapes(n_new, mx, 0, 0, int(interleaved), eps)
+    if some.dim() < 3 + (c.L > 0):
+        _refuse(2, "rows must be %s[B][new][heads][D] or packed" % ("[L]" if c.L else ""))
+    lead, n_new, mx = c.new_rows(some, "q" if k is None else "k", new_start, max_new)
+    H_q = rot = 0
+    qs = qos = ks = vs = _NO_STRIDES
     if q is not None:
-        s.H_q = q.shape[-2]
-        s.q = _row_strides(q, "q", k_pages, layers, lead, s.H_q, c.D)
-        s.q_out = _row_strides(q_out, "q_out", k_pages, layers, lead, s.H_q, c.D)
+        H_q = q.shape[-2]
+        qs, qos = c.rows(q, "q", lead, H_q), c.rows(q_out, "q_out", lead, H_q)
     if k is not None:
-        s.k = _row_strides(k, "k", k_pages, layers, lead, c.H_kv, c.D)
-        s.v = _row_strides(v, "v", k_pages, layers, lead, c.H_kv, c.D)
+        ks, vs = c.rows(k, "k", lead, c.heads), c.rows(v, "v", lead, c.heads)
     for name, g in (("q_gain", q_gain), ("k_gain", k_gain)):
-        if g is not None and (g.dtype != k_pages.dtype or g.get_device() != dev or g.numel() != c.L * c.D
+        if g is not None and (g.dtype is not c.dtype or g.get_device() != c.dev or g.numel() != (c.L or 1) * c.D
                               or not g.is_contiguous()):
             _refuse(2, "%s must be contiguous, [L][D], of the pools' type and device" % name)
     if inv_freq is not None:
-        if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.get_device() != dev:
+        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.get_device() != c.dev:
             _refuse(2, "inv_freq must be a contiguous float32 vector on the pools' device")
-        s.rotary_dim = 2 * inv_freq.numel()
-        if s.rotary_dim == 0:
+        rot = 2 * inv_freq.numel()
+        if rot == 0:
             _refuse(2, "inv_freq is empty")
-    if positions is not None:
-        _ints(positions, "positions", positions.dim(), dev, n_new)
-    r = _Rope(_ptr(q_gain), _ptr(k_gain), _ptr(inv_freq), _ptr(positions))
-    _check(load_library().mot_cache_append(_ptr(q), _ptr(k), _ptr(v), _ptr(q_out), _ptr(k_pages), _ptr(v_pages),
-                                           _ptr(table), _ptr(kv_len), _ptr(new_start), ctypes.byref(r), ctypes.byref(c),
-                                           ctypes.byref(s), torch.cuda.current_stream().cuda_stream))
-
-
-def _pages_scratch(c: _CacheShapes, n_rows: int, dev: int, workspace):
-    n = load_library().mot_cache_workspace_bytes(ctypes.byref(c), n_rows)
-    if n == ctypes.c_size_t(-1).value:
-        raise MotError(2, load_library().mot_last_error().decode())
-    held, nbytes = _scratch(n, dev, workspace, "workspace")
-    if held is None:
-        _refuse(1, "under a capture begun outside torch the call needs a workspace of %d bytes" % n)
-    return held, nbytes
+    pos = 0 if positions is None else c.ints(positions, "positions", positions.dim(), n_new)
+    rope = _ROPE.pack(0 if q_gain is None else q_gain.data_ptr(), 0 if k_gain is None else k_gain.data_ptr(),
+                      0 if inv_freq is None else inv_freq.data_ptr(), pos)
+    rc = lib.mot_cache_append(_ptr(q), _ptr(k), _ptr(v), _ptr(q_out), k_pages.data_ptr(), v_pages.data_ptr(),
+                              table.data_ptr(), kv, start, rope, c.packed,
+                              _APPEND.pack(n_new, mx, H_q, rot, interleaved, eps, *qs, *qos, *ks, *vs), _stream(c.dev))
+    if rc:
+        _check(rc)
 
 
 def cache_workspace_bytes(k_pages, v_pages, table, n_rows: int, page_layout: int = LAYOUT_BTHD) -> int:
     """Bytes of workspace of cache_reorder for n_rows new rows (0: of
     cache_compact)."""
-    c = _pools(k_pages, v_pages, table, page_layout)
-    n = load_library().mot_cache_workspace_bytes(ctypes.byref(c), n_rows)
-    if n == ctypes.c_size_t(-1).value:
-        raise MotError(2, load_library().mot_last_error().decode())
-    return int(n)
+    lib, _ = _ready()
+    return _sized(lib.mot_cache_workspace_bytes(_Pools(k_pages, v_pages, table, page_layout).packed, n_rows))
+
+
+def _pages_workspace(c: _Pools, n_rows: int, given) -> tuple:
+    need = _sized(_lib.mot_cache_workspace_bytes(c.packed, n_rows))
+    held, at, nbytes = c.scratch(need, given, "workspace")
+    if held is None:
+        _refuse(1, "under a capture begun outside torch the call needs a workspace of %d bytes" % need)
+    return held, at, nbytes
 
 
 def cache_reorder(k_pages, v_pages, table, source, keep, want, new_table, missing, page_layout: int = LAYOUT_BTHD,
@@ -697,33 +712,31 @@ def cache_reorder(k_pages, v_pages, table, source, keep, want, new_table, missin
     first keep[b] positions of row source[b] of table and room for want[b]
     (int32 [n_rows] each; missing: int32 [1], output).  workspace None: torch
     memory of this call."""
-    import torch
-    c = _pools(k_pages, v_pages, table, page_layout)
-    dev, n = k_pages.get_device(), source.numel()
-    for name, t in (("source", source), ("keep", keep), ("want", want)):
-        _ints(t, name, 1, dev, n)
-    _ints(new_table, "new_table", 2, dev, n * c.max_pages)
-    _ints(missing, "missing", 1, dev, 1)
-    if new_table.shape[0] != n:
-        _refuse(2, "new_table has %d rows, expected %d" % (new_table.shape[0], n))
-    held, nbytes = _pages_scratch(c, n, dev, workspace)
-    _check(load_library().mot_cache_reorder(_ptr(k_pages), _ptr(v_pages), _ptr(table), _ptr(source), _ptr(keep),
-                                            _ptr(want), _ptr(new_table), _ptr(missing), ctypes.byref(c), n, _ptr(held),
-                                            nbytes, torch.cuda.current_stream().cuda_stream))
+    lib, _ = _ready()
+    c = _Pools(k_pages, v_pages, table, page_layout)
+    n = source.numel()
+    src, kp, wt = c.ints(source, "source", 1), c.ints(keep, "keep", 1, n), c.ints(want, "want", 1, n)
+    new, short = c.ints(new_table, "new_table", 2), c.ints(missing, "missing", 1, 1)
+    if new_table.shape != (n, c.max_pages):
+        _refuse(2, "new_table has shape %s, expected %s" % (tuple(new_table.shape), (n, c.max_pages)))
+    held, at, nbytes = _pages_workspace(c, n, workspace)
+    rc = lib.mot_cache_reorder(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), src, kp, wt, new, short, c.packed,
+                               n, at, nbytes, _stream(c.dev))
+    if rc:
+        _check(rc)
 
 
 def cache_compact(k_pages, v_pages, table, new_table, used, page_layout: int = LAYOUT_BTHD, workspace=None) -> None:
     """mot_cache_compact on the current torch stream: the pages that table names
     move to the lowest numbers; new_table int32 like table and used int32 [1]
     are outputs.  workspace None: torch memory of this call."""
-    import torch
-    c = _pools(k_pages, v_pages, table, page_layout)
-    dev = k_pages.get_device()
-    _ints(new_table, "new_table", 2, dev, c.B * c.max_pages)
-    _ints(used, "used", 1, dev, 1)
+    lib, _ = _ready()
+    c = _Pools(k_pages, v_pages, table, page_layout)
+    new, n = c.ints(new_table, "new_table", 2), c.ints(used, "used", 1, 1)
     if new_table.shape != table.shape:
         _refuse(2, "new_table has shape %s, expected %s" % (tuple(new_table.shape), tuple(table.shape)))
-    held, nbytes = _pages_scratch(c, 0, dev, workspace)
-    _check(load_library().mot_cache_compact(_ptr(k_pages), _ptr(v_pages), _ptr(table), _ptr(new_table), _ptr(used),
-                                            ctypes.byref(c), _ptr(held), nbytes,
-                                            torch.cuda.current_stream().cuda_stream))
+    held, at, nbytes = _pages_workspace(c, 0, workspace)
+    rc = lib.mot_cache_compact(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), new, n, c.packed, at, nbytes,
+                               _stream(c.dev))
+    if rc:
+        _check(rc)

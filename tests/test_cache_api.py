@@ -90,15 +90,14 @@ def test_attention_no_ops(lib):
     assert _attend(n_new=0, max_new=0, ptrs=dict(q=None, o=None)) == "MOT_OK"
     assert _attend(cache=_cache(B=0), n_new=0, max_new=0, ptrs=dict(table=None, kv_len=None)) == "MOT_OK"
     s = mb._AttendShapes(1, 1, 4, 0, 0, 0.0, _rows(4, 64, 1), _rows(4, 64, 1))
-    with pytest.raises(mb.MotError):
-        mb.attend_workspace_bytes(_cache(D=80), s)
+    assert mb.load_library().mot_attend_workspace_bytes(ctypes.byref(_cache(D=80)), ctypes.byref(s)) == mb._SIZE_MAX
 
 
 def test_attention_workspace(lib):
     # a long decoding step is cut, and its workspace is checked where it is used
     c = _cache(B=1, max_pages=2048, H_kv=2)
     s = mb._AttendShapes(1, 1, 4, 0, 0, 0.0, _rows(4, 64, 1), _rows(4, 64, 1))
-    need = mb.attend_workspace_bytes(c, s)
+    need = mb.load_library().mot_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(s))
     assert need > 0 and need % 4 == 0
     free = FAKE + 40 * GIB
     kw = dict(cache=c, n_new=1, max_new=1, workspace_bytes=need)
@@ -196,6 +195,11 @@ def test_struct_layouts(tmp_path):
                     "/opt/rocm/include", str(src), "-o", str(tmp_path / "layout")], check=True)
     out = subprocess.run([str(tmp_path / "layout")], check=True, capture_output=True, text=True).stdout
     got = {tuple(x.split()[:2]): int(x.split()[2]) for x in out.splitlines()}
+    packed = {"mot_cache_shapes": mb._CACHE, "mot_append_shapes": mb._APPEND, "mot_rope": mb._ROPE}
+    for cname, st in packed.items():
+        assert st.size == got[(cname, "size")], cname
+    assert mb._ATTEND.size == got[("mot_attend_shapes", "workspace")]
+    assert mb._ATTEND.size + mb._SCRATCH.size == got[("mot_attend_shapes", "size")]
     for cname, cls in structs.items():
         assert got[(cname, "size")] == ctypes.sizeof(cls)
         for f, _ in cls._fields_:
