@@ -23,7 +23,8 @@ LIB = os.path.join(CSRC, "libmot.so")
 SOURCES = [(f, os.path.splitext(f)[0], {}) for f in
            ("mot_api.hip", "k_router.hip", "k_routed.hip", "k_f32.hip", "k_f32_split.hip", "k_bf16_unfused.hip", "k_bf16_gemm256.hip",
             "k_bf16_fused.hip", "k_project.hip", "k_replay.hip", "k_backbone.hip", "cache_api.hip", "k_cache.hip",
-            "k_paged_attn.hip")]
+            "k_paged_attn.hip",
+            "k_paged_decode.hip", "k_paged_chunk.hip", "k_paged_f32.hip")]
 SOURCES += [("k_bf16_fused_inst.hip", "k_bf16_fused_%d_%d" % (a, b),
              {"MOT_FUSED_D_IN": a, "MOT_FUSED_D_OUT": b})
             for a in (128, 256, 512) for b in (128, 256, 512)]
@@ -32,7 +33,7 @@ SOURCES += [("k_bf16_fused_inst.hip", "k_bf16_fused_%d_%d" % (a, b),
 # GEMM epilogues read them; the AGPR form copies them in and out)
 _VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 EXTRA = {f: _VGPR_FORM for f in ("k_replay.hip", "k_backbone.hip", "k_project.hip", "k_bf16_unfused.hip",
-                            "k_f32_split.hip", "k_paged_attn.hip")}
+                            "k_f32_split.hip", "k_paged_decode.hip", "k_paged_chunk.hip", "k_paged_f32.hip")}
 
 
 def hipcc() -> str:

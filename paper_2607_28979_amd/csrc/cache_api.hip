@@ -164,8 +164,7 @@ size_t mot_attend_workspace_bytes(const mot_cache_shapes* c, const mot_attend_sh
     if (check_attend(c, s, true) != MOT_OK) return SIZE_MAX;
     if (c->B == 0 || s->n_new == 0 || s->max_new == 0) return 0;
     AttendProblem p = attend_problem(c, s);
-    attend_cuts(p, c->dtype == MOT_BF16);
-    return attend_part_bytes(p);
+    return attend_plan(p, c->dtype == MOT_BF16);
 }
 
 mot_status mot_paged_attention(const void* q, const void* k_pages, const void* v_pages, const int32_t* table,
@@ -193,16 +192,12 @@ mot_status mot_paged_attention(const void* q, const void* k_pages, const void* v
     AttendProblem p = attend_problem(c, s);
     p.q = q; p.k = k_pages; p.v = v_pages; p.o = o;
     p.c.table = table; p.c.kv_len = kv_len; p.c.start = new_start;
-    attend_cuts(p, c->dtype == MOT_BF16);
-    const size_t need = attend_part_bytes(p);
+    const size_t need = attend_plan(p, c->dtype == MOT_BF16);
     if (need && s->workspace && s->workspace_bytes >= need) {
         if (!aligned16(s->workspace))
             return fail(MOT_ERR_MISALIGNED, "workspace %p is not 16-byte aligned", s->workspace);
         if ((st = apart({"workspace", s->workspace, need}, in, 7)) != MOT_OK) return st;
         p.part = reinterpret_cast<float*>(s->workspace);
-    } else {
-        p.n_split = 1;
-        p.split_len = c->max_pages * c->page_size;
     }
     return launched(launch_paged_attention(p, c->dtype == MOT_BF16, stream));
 }

@@ -52,9 +52,9 @@ struct AttendProblem {
     PageTable c;
     const void *q, *k, *v;
     void* o;
-    float* part;             // partial rows and their (maximum, sum), NULL: no cuts
+    float* part;             // partial sums, NULL: nothing is cut
     int32_t H_q, window;
-    int32_t split_len, n_split;
+    int32_t n_split, least;  // workgroups that share the work (1: they do not), blocks of a share at least
     int32_t max_kv;          // bound on kv_len that the cuts go by
     float scale_log2;        // scale * log2(e)
     RowStrides qs, os;
@@ -84,10 +84,14 @@ struct PagesProblem {
     void* ws;
 };
 
-// How a call's positions are cut: n_split of split_len each (1: not at all)
-void attend_cuts(AttendProblem& p, bool bf16);
-size_t attend_part_bytes(const AttendProblem& p);
+// Sets p.n_split and p.least; the bytes of `part` that they need (0: nothing is cut).
+size_t attend_plan(AttendProblem& p, bool bf16);
 hipError_t launch_paged_attention(const AttendProblem& p, bool bf16, hipStream_t stream);
+// bf16 calls whose sequences have a tile of 32 query rows at most per KV head
+// (k_paged_decode.hip), more (k_paged_chunk.hip), and fp32 ones (k_paged_f32.hip)
+hipError_t launch_paged_decode(const AttendProblem& p, hipStream_t stream);
+hipError_t launch_paged_chunk(const AttendProblem& p, hipStream_t stream);
+hipError_t launch_paged_f32(const AttendProblem& p, hipStream_t stream);
 hipError_t launch_cache_append(const AppendProblem& p, bool bf16, hipStream_t stream);
 size_t pages_workspace_bytes(int64_t n_pages, int64_t n_rows);
 hipError_t launch_cache_reorder(const PagesProblem& p, hipStream_t stream);
