@@ -617,7 +617,7 @@ mot_status mot_cache_append(const void* q, const void* k, const void* v, void* q
  *                are holes); 0 when the pool sufficed
  *   workspace    device scratch of this call, at least mot_cache_workspace_bytes
  *                (16-byte aligned, not overlapping its arrays; calls that
- *                overlap in time need their own)
+ *                overlap in time need their own); not looked at where that is 0
  * Beam search sets source to the parents and want = keep + 1; a beam that ends
  * has source -1.  n_rows at most 4096 (0: a no-op that writes nothing).  The
  * data of pages that new rows take over does not move.
@@ -641,7 +641,8 @@ mot_status mot_cache_compact(void* k_pages, void* v_pages, const int32_t* table,
                              hipStream_t stream);
 
 /* Scratch bytes of mot_cache_reorder for n_rows new rows (n_rows 0: of
- * mot_cache_compact); SIZE_MAX for invalid shapes. */
+ * mot_cache_compact); 0 for small pools and tables; SIZE_MAX for invalid
+ * shapes. */
 size_t mot_cache_workspace_bytes(const mot_cache_shapes* cache, int32_t n_rows);
 
 /* MOT_ABI_VERSION of the loaded library. */

@@ -565,8 +565,6 @@ class _Pools:
         st = t.stride()
         if st[-1] != 1 and self.D > 1:
             _refuse(2, "%s has a stride of %d between a head's elements" % (name, st[-1]))
-        if 1 in want:       # an axis of one entry may have any stride
-            st = tuple(0 if n == 1 else x for x, n in zip(st, want))
         return (st[0] if self.L else 0, st[-4] if len(lead) == 2 else 0, st[-3], st[-2])
 
     def new_rows(self, t, name: str, new_start, max_new) -> tuple:
@@ -701,7 +699,7 @@ def cache_workspace_bytes(k_pages, v_pages, table, n_rows: int, page_layout: int
 def _pages_workspace(c: _Pools, n_rows: int, given) -> tuple:
     need = _sized(_lib.mot_cache_workspace_bytes(c.packed, n_rows))
     held, at, nbytes = c.scratch(need, given, "workspace")
-    if held is None:
+    if held is None and need:
         _refuse(1, "under a capture begun outside torch the call needs a workspace of %d bytes" % need)
     return held, at, nbytes
 

@@ -68,16 +68,19 @@ mot_status check_rows(const mot_cache_shapes* c, int n_new, int max_new, bool pa
 mot_status check_strides(const char* name, const mot_strides& s, const mot_cache_shapes* c, int n_new, int max_new,
                          int heads, int layers, bool packed, size_t* bytes) {
     const int64_t v[4] = {s.layer, s.batch, s.token, s.head}, m = c->dtype == MOT_BF16 ? 8 : 4;
+    // an axis of one entry may have any stride
+    const int64_t n[4] = {layers, packed ? 1 : c->B, packed ? n_new : max_new, heads};
+    int64_t at = c->D;   // of the last element, and one
+    double far = c->D;
     for (int i = 0; i < 4; ++i) {
-        if ((i == 0 && layers == 1) || (i == 1 && packed)) continue;   // not used
+        if (n[i] <= 1) continue;
         if (v[i] < 0 || v[i] > (int64_t)1 << 40) return fail(MOT_ERR_BAD_SHAPE, "a stride of %s is negative or above 2^40", name);
         if (v[i] % m) return fail(MOT_ERR_MISALIGNED, "a stride of %s is not a multiple of 16 bytes", name);
+        far += (double)(n[i] - 1) * v[i];
+        at += (n[i] - 1) * v[i];
     }
-    const double last = (double)(layers - 1) * s.layer + (packed ? 0.0 : (double)(c->B - 1) * s.batch) +
-                        (double)((packed ? n_new : max_new) - 1) * s.token + (double)(heads - 1) * s.head + c->D;
-    if (last > 9e18 / 8) return fail(MOT_ERR_BAD_SHAPE, "%s spans more than the address space", name);
-    *bytes = (size_t)((layers > 1 ? (layers - 1) * s.layer : 0) + (packed ? 0 : (c->B - 1) * s.batch) +
-                      ((packed ? n_new : max_new) - 1) * s.token + (heads - 1) * s.head + c->D) * elem(c);
+    if (far > 1e18) return fail(MOT_ERR_BAD_SHAPE, "%s spans more than the address space", name);
+    *bytes = (size_t)at * elem(c);
     return MOT_OK;
 }
 
@@ -243,7 +246,8 @@ mot_status mot_cache_append(const void* q, const void* k, const void* v, void* q
     const bool same = q && q == q_out;
     if (same) {
         const mot_strides &a = s->q, &b = s->q_out;
-        if ((c->L > 1 && a.layer != b.layer) || (!packed && a.batch != b.batch) || a.token != b.token || a.head != b.head)
+        if ((c->L > 1 && a.layer != b.layer) || (!packed && c->B > 1 && a.batch != b.batch) ||
+            ((packed ? s->n_new : s->max_new) > 1 && a.token != b.token) || (s->H_q > 1 && a.head != b.head))
             return fail(MOT_ERR_BAD_SHAPE, "q_out is q with other strides");
     }
     const size_t pb = k ? pool_bytes(c) * c->L : 0, gb = (size_t)c->L * c->D * elem(c);
@@ -280,7 +284,7 @@ size_t mot_cache_workspace_bytes(const mot_cache_shapes* c, int32_t n_rows) {
         fail(MOT_ERR_BAD_SHAPE, "n_rows=%d must be in [0, 4096]", n_rows);
         return SIZE_MAX;
     }
-    return pages_workspace_bytes(c->n_pages, n_rows);
+    return pages_workspace_bytes(c->n_pages, n_rows, n_rows ? n_rows : c->B, c->max_pages);
 }
 
 }  // extern "C"
@@ -291,14 +295,15 @@ namespace {
 mot_status pages_call(void* k_pages, void* v_pages, const int32_t* table, const int32_t* source, const int32_t* keep,
                       const int32_t* want, int32_t* new_table, int32_t* count, const mot_cache_shapes* c, int32_t n_rows,
                       bool reorder, void* ws, size_t ws_bytes, hipStream_t stream) {
-    if (!k_pages || !v_pages || !new_table || !count || !ws || (!table && c->B) || (reorder && (!source || !keep || !want)))
+    if (!k_pages || !v_pages || !new_table || !count || (!table && c->B) || (reorder && (!source || !keep || !want)))
         return fail(MOT_ERR_NULL_ARG, "a required argument is NULL");
-    for (const void* x : {(const void*)k_pages, (const void*)v_pages, (const void*)ws})
+    const size_t need = pages_workspace_bytes(c->n_pages, reorder ? n_rows : 0, reorder ? n_rows : c->B, c->max_pages);
+    if (need && !ws) return fail(MOT_ERR_NULL_ARG, "a workspace of %zu bytes is required", need);
+    if (ws_bytes < need) return fail(MOT_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, need %zu", ws_bytes, need);
+    for (const void* x : {(const void*)k_pages, (const void*)v_pages, need ? (const void*)ws : nullptr})
         if (!aligned16(x)) return fail(MOT_ERR_MISALIGNED, "device pointer %p is not 16-byte aligned", x);
     for (const int32_t* x : {table, source, keep, want, (const int32_t*)new_table, (const int32_t*)count})
         if (!aligned4(x)) return fail(MOT_ERR_MISALIGNED, "device pointer %p is not 4-byte aligned", (const void*)x);
-    const size_t need = pages_workspace_bytes(c->n_pages, reorder ? n_rows : 0);
-    if (ws_bytes < need) return fail(MOT_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, need %zu", ws_bytes, need);
     const size_t rows = reorder ? n_rows : c->B, pb = pool_bytes(c) * c->L;
     const Extent all[] = {{"k_pages", k_pages, pb}, {"v_pages", v_pages, pb}, {"new_table", new_table, rows * c->max_pages * 4},
                           {"the count", count, 4}, {"workspace", ws, need},

@@ -93,7 +93,9 @@ hipError_t launch_paged_decode(const AttendProblem& p, hipStream_t stream);
 hipError_t launch_paged_chunk(const AttendProblem& p, hipStream_t stream);
 hipError_t launch_paged_f32(const AttendProblem& p, hipStream_t stream);
 hipError_t launch_cache_append(const AppendProblem& p, bool bf16, hipStream_t stream);
-size_t pages_workspace_bytes(int64_t n_pages, int64_t n_rows);
+// n_rows: of a reordering, 0: compaction; rows x max_pages: entries of the new table (0 bytes:
+// the plan fits a workgroup's LDS)
+size_t pages_workspace_bytes(int64_t n_pages, int64_t n_rows, int64_t rows, int64_t max_pages);
 hipError_t launch_cache_reorder(const PagesProblem& p, hipStream_t stream);
 hipError_t launch_cache_compact(const PagesProblem& p, hipStream_t stream);
 

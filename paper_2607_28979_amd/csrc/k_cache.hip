@@ -348,10 +348,52 @@ __global__ __launch_bounds__(kThreads) void k_pages_squeeze(PagesProblem p, Page
     }
 }
 
-constexpr int kCopyBytes = 16384;   // of one work item
+constexpr int kCopyChunks = 1024;   // 16-byte chunks of one copying work item at most
 
-// The new table (the first `tables` workgroups), and the copies: work items are
-// pieces of kCopyBytes of a page of a layer's keys or values.
+// Work item `it` of the copies of a call, by THREADS threads of which this is `tid`: a piece of
+// a page of a layer's keys or values.  pair(c): pages from and to, and the positions to
+// copy (0: all).  Four chunks per thread are under way at a time.
+template <int THREADS, class Pair>
+__device__ __forceinline__ void copy_item(const PagesProblem& p, int64_t it, int pieces, int tid, Pair pair) {
+    // in 32 bits: the pools of 2^31 pages or pieces would not fit in the device's memory
+    const uint32_t i0 = __builtin_amdgcn_readfirstlane((uint32_t)it), i1 = i0 / (uint32_t)pieces, i2 = i1 / (2u * p.L);
+    const int piece = (int)(i0 - i1 * pieces), side = (int)(i1 - i2 * 2u * p.L);
+    const int4 pr = pair((int)i2);
+    if (pr.y < 0) return;
+    const int64_t page_bytes = p.c.page_elems * p.elem_bytes, row_bytes = (int64_t)p.c.D * p.elem_bytes;
+    // contiguous bytes: of each head where the heads come first
+    int64_t run = page_bytes, pitch = 0;
+    int runs = 1;
+    if (pr.z && p.heads_first) {
+        run = pr.z * row_bytes;
+        runs = p.c.H_kv;
+        pitch = row_bytes << p.c.page_shift;
+    } else if (pr.z) {
+        run = pr.z * row_bytes * p.c.H_kv;
+    }
+    char* pool = reinterpret_cast<char*>(side & 1 ? p.v_pages : p.k_pages) + (int64_t)(side >> 1) * p.c.n_pages * page_bytes;
+    const char* from = pool + pr.x * page_bytes;
+    char* to = pool + pr.y * page_bytes;
+    const int chunks = (int)(run / 16), end = min((piece + 1) * kCopyChunks, chunks * runs);
+    for (int x0 = piece * kCopyChunks + tid; x0 < end; x0 += 4 * THREADS) {
+        u32x4 v[4];
+        int64_t off[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int x = x0 + i * THREADS, y = runs > 1 ? x / chunks : 0;
+            off[i] = y * pitch + (int64_t)(x - y * chunks) * 16;
+            if (x < end) v[i] = *reinterpret_cast<const u32x4*>(from + off[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (x0 + i * THREADS < end) *reinterpret_cast<u32x4*>(to + off[i]) = v[i];
+    }
+}
+__host__ __device__ inline int copy_pieces(const PagesProblem& p) {
+    return (int)((p.c.page_elems * p.elem_bytes / 16 + kCopyChunks - 1) / kCopyChunks);
+}
+
+// The new table (the first `tables` workgroups), and the copies.
 __global__ __launch_bounds__(256) void k_pages_apply(PagesProblem p, PagesWs w, int tables) {
     const int tid = threadIdx.x, M = p.c.max_pages;
     if ((int)blockIdx.x < tables) {
@@ -386,44 +428,217 @@ __global__ __launch_bounds__(256) void k_pages_apply(PagesProblem p, PagesWs w, 
         p.new_table[at] = page;
         return;
     }
-    const int n = *w.n_pair, sides = 2 * p.L;
-    const int64_t page_bytes = p.c.page_elems * p.elem_bytes;
-    const int pieces = (int)((page_bytes + kCopyBytes - 1) / kCopyBytes);
-    const int64_t items = (int64_t)n * sides * pieces;
-    const int64_t row_bytes = (int64_t)p.c.D * p.elem_bytes;
-    for (int64_t it = blockIdx.x - tables; it < items; it += gridDim.x - tables) {
-        const int piece = (int)(it % pieces), side = (int)(it / pieces % sides), c = (int)(it / pieces / sides);
-        int src, dst;
-        int64_t run = page_bytes;   // contiguous bytes, of each head where the heads come first
-        int runs = 1;
-        int64_t pitch = 0;
-        if (p.n_rows) {
-            const int4 pr = w.pair[c];
-            src = pr.x;
-            dst = pr.y;
-            if (dst < 0) continue;
-            if (p.heads_first) {
-                run = pr.z * row_bytes;
-                runs = p.c.H_kv;
-                pitch = row_bytes << p.c.page_shift;
-            } else {
-                run = pr.z * row_bytes * p.c.H_kv;
+    const int pieces = copy_pieces(p);
+    const int64_t items = (int64_t)*w.n_pair * 2 * p.L * pieces;
+    for (int64_t it = blockIdx.x - tables; it < items; it += gridDim.x - tables)
+        copy_item<256>(p, it, pieces, tid, [&](int c) { return p.n_rows ? w.pair[c] : make_int4(w.from[c], w.list[c], 0, 0); });
+}
+
+// ---- small pools and tables: one launch -----------------------------------------
+//
+// Every workgroup works out the whole plan in its own LDS, from the table and the rows
+// (L2 holds them), and then does its share of the new table and of the copies: no
+// workspace, no order between workgroups. All 16 waves of a CU run the plan, so an
+// instruction more in its loops is felt (16 cycles per 1024 threads): a wave walks rows,
+// not entries, and what a row says stays in scalars (entry by entry the reorder of 200 rows
+// took 22 us). Against the launches above, replayed from a graph: 200 rows of 123 entries,
+// 9015 pages, few copies 12.3 and 16.7 us; 64 rows of 39, 22 MB moved 11.8 and 18.6; a pool
+// of 101 pages squeezed 7.8 and 14.7, one of 2096 pages x 14 layers (909 MB moved) 191
+// (4.8 TB/s) and 201. At the limits, 16384 pages and 512 rows of 128: reorder 16.0 and 14.1,
+// compaction 18.8 and 21.5 (4 rows of 16384: 26.5 and 14.3, 29.9 and 21.3), but issuing from
+// the host 7 and 16 us.
+
+constexpr int kOncePages = 16384, kOnceRows = 512, kOnceEntries = 65536;
+constexpr int kOnceGrid = 256;   // a workgroup per CU
+constexpr int kWaves = kThreads / 64;
+
+// f(page, row, j) for the entries j < count(b) of rows b of a table of `rows` rows of M
+// (row b reads row source(b)); a page out of range is skipped. A wave takes rows w, w + 16,
+// ..., 8 rows x 128 entries of loads under way together; with fewer than 16 rows the waves
+// share a row's entries.
+template <class Source, class Count, class Use>
+__device__ __forceinline__ void each_page(const int32_t* table, int N, int rows, int M, int wave, Source source, Count count,
+                                          Use use) {
+    constexpr int kRows = 8, kCuts = 2;
+    const int lane = threadIdx.x & 63;
+    const int share = rows >= kWaves ? 0 : 4 - (31 - __clz(rows));   // 2^share waves to a row
+    const int step = kWaves >> share, b0 = wave >> share, cut0 = wave & ((1 << share) - 1);
+    for (int bb = b0; bb < rows; bb += kRows * step) {
+        for (int j0 = 64 * kCuts * cut0; j0 < M; j0 += 64 * kCuts << share) {
+            int v[kRows * kCuts];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const int32_t* t = table + (int64_t)source(min(bb + r * step, rows - 1)) * M;
+#pragma unroll
+                for (int k = 0; k < kCuts; ++k) v[r * kCuts + k] = t[min(j0 + 64 * k + lane, M - 1)];
             }
-        } else {
-            src = w.from[c];
-            dst = w.list[c];
-        }
-        char* pool = reinterpret_cast<char*>(side & 1 ? p.v_pages : p.k_pages) + (int64_t)(side >> 1) * p.c.n_pages * page_bytes;
-        const char* from = pool + src * page_bytes;
-        char* to = pool + dst * page_bytes;
-        const int chunks = (int)(run / 16);   // 16-byte chunks of a run
-        const int end = min((piece + 1) * (kCopyBytes / 16), chunks * runs);
-        for (int x = piece * (kCopyBytes / 16) + tid; x < end; x += 256) {
-            const int y = x / chunks;
-            const int64_t off = y * pitch + (int64_t)(x - y * chunks) * 16;
-            *reinterpret_cast<u32x4*>(to + off) = *reinterpret_cast<const u32x4*>(from + off);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const int b = bb + r * step;
+                if (b >= rows) break;
+                const int n = count(b);
+#pragma unroll
+                for (int k = 0; k < kCuts; ++k) {
+                    const int j = j0 + 64 * k + lane, page = v[r * kCuts + k];
+                    if (j < n && (uint32_t)page < (uint32_t)N) use(page, b, j);
+                }
+            }
         }
     }
+}
+
+struct OnceRow {
+    int src, full, kept, need, rest, base, copied, spare;
+};
+
+// Bits of the words of mark[N] that are not 0, 32 to a word, by all threads. words: at
+// least 2 * ceil(N / 64).
+__device__ __forceinline__ void bits_of(const uint32_t* mark, int N, uint32_t* words, int wave) {
+    const int lane = threadIdx.x & 63;
+    for (int g = wave; 64 * g < N; g += kWaves) {
+        const int i = 64 * g + lane;
+        const uint64_t m = __ballot(i < N && mark[min(i, N - 1)] != 0);
+        if (lane < 2) words[2 * g + lane] = (uint32_t)(m >> (32 * lane));
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void k_pages_reorder(PagesProblem p) {
+    // a word per page: 0 free, ~0 kept whole by a row, else kept in part and the lowest
+    // such row b as kOnceRows - b; once this is read, the free pages in order
+    __shared__ __attribute__((aligned(16))) uint32_t mark[kOncePages];
+    __shared__ OnceRow row[kOnceRows];
+    __shared__ int4 pair[kOnceRows];
+    __shared__ int last[kOnceRows];   // the page kept in part, -1: none
+    __shared__ uint32_t held[kOncePages / 32 + 2];
+    __shared__ int s_wave[kWaves];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int M = p.c.max_pages, N = p.c.n_pages, W = (N + 31) / 32, R = p.n_rows;
+    for (int i = tid; i < (N + 3) / 4; i += kThreads) reinterpret_cast<u32x4*>(mark)[i] = u32x4{};
+    if (tid < R) {
+        const RowPlan r = row_plan(p, tid);
+        row[tid] = OnceRow{r.src, r.full, r.kept, r.need, r.rest, 0, 0, 0};
+        last[tid] = -1;
+    }
+    __syncthreads();
+    if (p.c.B > 0) each_page(   // a table without rows is not read
+        p.c.table, N, R, M, wave, [&](int b) { return __builtin_amdgcn_readfirstlane(row[b].src); },
+        [&](int b) { return __builtin_amdgcn_readfirstlane(row[b].kept); },
+        [&](int page, int b, int j) {
+            // ~0 is the largest word, so a plain store and the maximum agree in any order
+            if (j < row[b].full) {
+                mark[page] = ~0u;
+            } else {
+                atomicMax(mark + page, (uint32_t)(kOnceRows - b));
+                last[b] = page;
+            }
+        });
+    __syncthreads();
+    bits_of(mark, N, held, wave);
+    // a row copies its last page if another keeps it whole, or a lower row in part
+    int copied = 0, need = 0, sums;
+    if (tid < R) {
+        const int mine = last[tid];
+        copied = mine >= 0 && mark[mine] != (uint32_t)(kOnceRows - tid);
+        need = copied + max(row[tid].need - row[tid].kept, 0);
+    }
+    // both sums in one scan: at most kOnceEntries + kOnceRows pages, kOnceRows copies
+    static_assert(kOnceEntries + kOnceRows < 1 << 20 && kOnceRows < 1 << 11, "");
+    const int before = block_scan(copied << 20 | need, s_wave, &sums);
+    const int at = before & ((1 << 20) - 1), c = before >> 20, asked = sums & ((1 << 20) - 1), copies = sums >> 20;
+    if (tid < R) {
+        row[tid].base = at;
+        row[tid].copied = copied;
+        if (copied) pair[c] = make_int4(last[tid], at, row[tid].rest, 0);   // its place in the list, for now
+    }
+    int* list = reinterpret_cast<int*>(mark);
+    int n_free;
+    {
+        uint32_t f = tid < W ? ~held[tid] : 0u;   // W <= kThreads
+        if (tid == W - 1 && (N & 31)) f &= (1u << (N & 31)) - 1u;
+        int to = block_scan(__popc(f), s_wave, &n_free);
+        for (; f && to < asked; f &= f - 1, ++to) list[to] = 32 * tid + __ffs(f) - 1;
+    }
+    __syncthreads();
+    const int given = min(asked, n_free);
+    if (blockIdx.x == 0 && tid == 0) *p.count = asked - given;
+    for (int e = blockIdx.x + gridDim.x * tid; e < R * M; e += gridDim.x * kThreads) {
+        const int b = e / M, j = e - b * M;
+        const OnceRow r = row[b];
+        int page = j < r.kept ? p.c.table[(int64_t)r.src * M + j] : -1, ask = -1;
+        if ((uint32_t)page >= (uint32_t)N) page = -1;
+        if (r.copied && j == r.full) ask = r.base;
+        else if (j >= r.kept && j < r.need) ask = r.base + r.copied + j - r.kept;
+        p.new_table[e] = ask < 0 ? page : ask < given ? list[ask] : -1;
+    }
+    const int pieces = copy_pieces(p);
+    const int64_t items = (int64_t)copies * 2 * p.L * pieces;
+    for (int64_t it = blockIdx.x + gridDim.x * (tid >> 8); it < items; it += gridDim.x * (kThreads >> 8))
+        copy_item<256>(p, it, pieces, tid & 255, [&](int i) {
+            const int4 x = pair[i];
+            return make_int4(x.x, x.y < given ? list[x.y] : -1, x.z, 0);
+        });
+}
+
+__global__ __launch_bounds__(kThreads) void k_pages_compact(PagesProblem p) {
+    // a word per page, not 0: held; once this is read, pages to move and their places
+    __shared__ __attribute__((aligned(16))) uint32_t mark[kOncePages + 4];
+    // held as bits, and the held pages before each of its words
+    __shared__ uint32_t held[kOncePages / 32 + 2];
+    __shared__ int rank[kOncePages / 32 + 1];
+    __shared__ int s_wave[kWaves];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int M = p.c.max_pages, N = p.c.n_pages, W = (N + 31) / 32;
+    int* from = reinterpret_cast<int*>(mark);
+    int* list = from + N / 2 + 1;
+    for (int i = tid; i < (N + 3) / 4; i += kThreads) reinterpret_cast<u32x4*>(mark)[i] = u32x4{};
+    __syncthreads();
+    each_page(p.c.table, N, p.c.B, M, wave, [](int b) { return b; }, [&](int) { return M; },
+              [&](int page, int, int) { mark[page] = 1; });
+    __syncthreads();
+    bits_of(mark, N, held, wave);
+    __syncthreads();
+    int used;
+    const uint32_t h = tid < W ? held[tid] : 0u;
+    const int before = block_scan(__popc(h), s_wave, &used);
+    for (int i = tid; i <= W; i += kThreads) rank[i] = i < W ? before : used;   // W <= kThreads
+    if (tid == 0) held[W] = 0;
+    __syncthreads();
+    // held pages before page `used`: those that stay (word W, past the last, holds none)
+    const int stay = rank[used >> 5] + __popc(held[used >> 5] & ((1u << (used & 31)) - 1u));
+    if (tid < W) {
+        const int first = 32 * tid;
+        // holes below `used` and held pages from there on: a word has few of either
+        const uint32_t all = first + 32 <= N ? ~0u : (1u << (N - first)) - 1u;
+        const uint32_t low = first + 32 <= used ? ~0u : first >= used ? 0u : (1u << (used - first)) - 1u;
+        for (uint32_t m = ~h & all & low; m; m &= m - 1) {
+            const int k = __ffs(m) - 1;
+            list[first + k - before - __popc(h & ((1u << k) - 1u))] = first + k;
+        }
+        int n = before + __popc(h & low) - stay;
+        for (uint32_t m = h & ~low; m; m &= m - 1) from[n++] = first + __ffs(m) - 1;
+    }
+    __syncthreads();
+    if (blockIdx.x == 0 && tid == 0) *p.count = used;
+    for (int e = blockIdx.x + gridDim.x * tid; e < p.c.B * M; e += gridDim.x * kThreads) {
+        int page = p.c.table[e];
+        if ((uint32_t)page >= (uint32_t)N) page = -1;
+        else if (page >= used) page = list[rank[page >> 5] + __popc(held[page >> 5] & ((1u << (page & 31)) - 1u)) - stay];
+        p.new_table[e] = page;
+    }
+    const int pieces = copy_pieces(p);
+    const int64_t items = (int64_t)(used - stay) * 2 * p.L * pieces;
+    for (int64_t it = blockIdx.x + gridDim.x * (tid >> 8); it < items; it += gridDim.x * (kThreads >> 8))
+        copy_item<256>(p, it, pieces, tid & 255, [&](int i) { return make_int4(from[i], list[i], 0, 0); });
+}
+
+bool once(int64_t n_pages, int64_t n_rows, int64_t rows, int64_t max_pages) {
+    return n_pages <= kOncePages && n_rows <= kOnceRows && rows * max_pages <= kOnceEntries;
+}
+
+hipError_t launch_once(const PagesProblem& p, hipStream_t stream) {
+    if (p.n_rows) k_pages_reorder<<<kOnceGrid, kThreads, 0, stream>>>(p);
+    else k_pages_compact<<<kOnceGrid, kThreads, 0, stream>>>(p);
+    return hipGetLastError();
 }
 
 hipError_t pages_apply(const PagesProblem& p, const PagesWs& w, hipStream_t stream) {
@@ -448,9 +663,12 @@ hipError_t launch_cache_append(const AppendProblem& p, bool bf16, hipStream_t st
     return bf16 ? append_as<uint16_t>(p, stream) : append_as<float>(p, stream);
 }
 
-size_t pages_workspace_bytes(int64_t n_pages, int64_t n_rows) { return 4 * ws_words(n_pages, n_rows, nullptr, nullptr); }
+size_t pages_workspace_bytes(int64_t n_pages, int64_t n_rows, int64_t rows, int64_t max_pages) {
+    return once(n_pages, n_rows, rows, max_pages) ? 0 : 4 * ws_words(n_pages, n_rows, nullptr, nullptr);
+}
 
 hipError_t launch_cache_reorder(const PagesProblem& p, hipStream_t stream) {
+    if (once(p.c.n_pages, p.n_rows, p.n_rows ? p.n_rows : p.c.B, p.c.max_pages)) return launch_once(p, stream);
     PagesWs w;
     ws_words(p.c.n_pages, p.n_rows, p.ws, &w);
     hipError_t e = pages_mark(p, w, stream);
@@ -461,6 +679,7 @@ hipError_t launch_cache_reorder(const PagesProblem& p, hipStream_t stream) {
 }
 
 hipError_t launch_cache_compact(const PagesProblem& p, hipStream_t stream) {
+    if (once(p.c.n_pages, p.n_rows, p.n_rows ? p.n_rows : p.c.B, p.c.max_pages)) return launch_once(p, stream);
     PagesWs w;
     ws_words(p.c.n_pages, 0, p.ws, &w);
     hipError_t e = pages_mark(p, w, stream);

@@ -163,13 +163,14 @@ def test_pages_refuse(lib, fn):
     assert _pages(fn, k=None) == "MOT_ERR_NULL_ARG"
     assert _pages(fn, new=None) == "MOT_ERR_NULL_ARG"
     assert _pages(fn, count=None) == "MOT_ERR_NULL_ARG"
-    assert _pages(fn, ws=None) == "MOT_ERR_NULL_ARG"
-    assert _pages(fn, ws_bytes=64) == "MOT_ERR_WORKSPACE_TOO_SMALL"
-    assert _pages(fn, ws=FAKE + 20 * GIB + 4) == "MOT_ERR_MISALIGNED"
+    big = _cache(n_pages=20000)      # small ones need no workspace
+    assert _pages(fn, cache=big, ws=None) == "MOT_ERR_NULL_ARG"
+    assert _pages(fn, cache=big, ws_bytes=64) == "MOT_ERR_WORKSPACE_TOO_SMALL"
+    assert _pages(fn, cache=big, ws=FAKE + 20 * GIB + 4) == "MOT_ERR_MISALIGNED"
+    assert _pages(fn, cache=big, ws=FAKE + 64) == "MOT_ERR_BAD_SHAPE"
     assert _pages(fn, table=FAKE + 2 * GIB + 1) == "MOT_ERR_MISALIGNED"
     assert _pages(fn, new=FAKE + 2 * GIB) == "MOT_ERR_BAD_SHAPE"           # in place
     assert _pages(fn, v=FAKE + 4096) == "MOT_ERR_BAD_SHAPE"
-    assert _pages(fn, ws=FAKE + 64) == "MOT_ERR_BAD_SHAPE"
     assert _pages(fn, count=FAKE) == "MOT_ERR_BAD_SHAPE"
     assert _pages(fn, cache=_cache(page_size=17)) == "MOT_ERR_UNSUPPORTED"
     assert _pages(fn, cache=_cache(L=300)) == "MOT_ERR_BAD_SHAPE"

@@ -427,7 +427,9 @@ REORDER = [  # rows, new rows, entries per row, page, H, D, type, layout, layers
     (6, 6, 5, 16, 2, 64, "bf16", 0, 3, 40), (6, 9, 5, 16, 2, 64, "bf16", 1, 2, 40), (1, 1, 1, 16, 1, 16, "bf16", 0, 1, 1),
     (8, 3, 4, 32, 1, 128, "f32", 0, 2, 2), (5, 30, 6, 16, 2, 64, "bf16", 0, 1, 4),   # more than there is
     (40, 50, 7, 16, 1, 16, "f32", 1, 2, 200), (3, 1100, 2, 16, 1, 16, "bf16", 0, 1, 3000),
-    (70, 70, 300, 16, 1, 16, "bf16", 0, 1, 400), (2, 4096, 1, 16, 1, 16, "bf16", 0, 1, 4096)]
+    (70, 70, 300, 16, 1, 16, "bf16", 0, 1, 400), (2, 4096, 1, 16, 1, 16, "bf16", 0, 1, 4096),
+    (20, 512, 3, 16, 1, 16, "bf16", 1, 1, 1000), (20, 513, 3, 32, 2, 16, "f32", 1, 2, 1000), (300, 40, 1700, 16, 1, 16, "bf16", 0, 1, 10),
+    (9, 9, 4, 16, 1, 16, "bf16", 1, 2, 16500)]
 
 
 @pytest.mark.parametrize("case", REORDER, ids=lambda c: "-".join(map(str, c)))
@@ -467,7 +469,9 @@ def test_reorder_from_no_rows():
 COMPACT = [  # rows, entries, page, H, D, type, layout, layers, pages of the pool, share held
     (4, 6, 16, 2, 64, "bf16", 0, 3, 30, 0.5), (4, 6, 16, 2, 64, "f32", 1, 2, 24, 0.9), (1, 1, 16, 1, 16, "bf16", 0, 1, 1, 1.0),
     (3, 3, 32, 1, 128, "bf16", 0, 1, 64, 0.0), (8, 8, 16, 1, 16, "bf16", 0, 1, 64, 1.0), (50, 64, 16, 1, 16, "bf16", 0, 2, 3300, 0.4),
-    (200, 40, 16, 1, 16, "f32", 0, 1, 40000, 0.7)]
+    (200, 40, 16, 1, 16, "f32", 0, 1, 40000, 0.7),
+    (30, 40, 16, 2, 16, "bf16", 1, 2, 16384, 0.9), (30, 40, 16, 2, 16, "bf16", 1, 2, 16385, 0.9), (700, 100, 16, 1, 16, "bf16", 0, 1, 16000, 0.2),
+    (2, 600, 16, 1, 16, "bf16", 0, 1, 1024, 0.85)]
 
 
 @pytest.mark.parametrize("case", COMPACT, ids=lambda c: "-".join(map(str, c)))
@@ -659,7 +663,7 @@ def test_binding_refuses():
             mb.cache_append(**{**good, **change})
     new, one = torch.empty_like(c.d_table), _i32([0])
     for change in (dict(new_table=new[:1]), dict(new_table=c.d_table), dict(missing=_i32([0, 0])), dict(keep=_i32([1])),
-                   dict(workspace=torch.empty(16, dtype=torch.uint8, device="cuda")), dict(source=_i32([0, 1]).long())):
+                   dict(workspace=torch.empty(16, dtype=torch.uint8)), dict(source=_i32([0, 1]).long())):
         with pytest.raises(mb.MotError):
             mb.cache_reorder(**{**dict(k_pages=c.k, v_pages=c.v, table=c.d_table, source=_i32([0, 1]), keep=_i32([1, 1]),
                                        want=_i32([1, 1]), new_table=new, missing=one), **change})
