@@ -41,6 +41,10 @@ constexpr int kMostTokens = 4;   // tokens of a workgroup
 // both elements of a half-split pair are in one lane.  Angles are shared by a
 // token's heads: computed once per workgroup, into LDS; position * inv_freq in
 // fp64, since fp32 leaves an error of 2e-3 turns at position 32768.
+// Bound: bytes for long prompts (4096 tokens of 28 + 2 x 4 heads of 128, 75 MB: 17 us of
+// which 3.5 are the launch; 28 layers of 1501 tokens, 172 MB: 37 us, 4.7 TB/s), the launch
+// and one chain of loads for single tokens (32 sequences: 5 us).  Rows two at a time, for
+// more loads under way, took 108 registers and 10 to 25 % longer.
 //
 // grid (ceil(max_new / tpb), B, L), 256 threads
 template <typename T, int LPR>
@@ -149,14 +153,18 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendProblem p, int tpb) 
 
 template <typename T>
 hipError_t append_as(const AppendProblem& p, hipStream_t stream) {
-    // one token per workgroup until there are several for every CU
+    // Tokens of a workgroup: one until there are several for every CU, then four where four
+    // tokens' heads are one turn of its threads, else two.  Measured (us with 1, 2, 4 tokens,
+    // heads of 128): 36 heads, 512 tokens 5.4, 6.2, 7.8; 2048: 11.8, 11.1, 12.2; 8192: 38,
+    // 37, 42; 8 heads, 1800 tokens 4.6, 4.2, 4.1; 42000: 51, 42, 37 (8 tokens: 39).
     const int64_t tokens = (int64_t)p.c.max_new * p.c.B * p.L;
-    const int tpb = tokens >= 2048 ? kMostTokens : 1;
+    const int lanes = p.c.D >> 4, lpr = lanes <= 2 ? 2 : lanes <= 4 ? 4 : lanes <= 8 ? 8 : 16;
+    const int heads = (p.q ? p.H_q : 0) + (p.k ? 2 * p.c.H_kv : 0);
+    const int tpb = tokens < 1792 ? 1 : kMostTokens * heads * lpr <= 256 ? kMostTokens : 2;
     const dim3 grid((p.c.max_new + tpb - 1) / tpb, p.c.B, p.L);
-    const int lanes = p.c.D >> 4;
-    if (lanes <= 2) k_cache_append<T, 2><<<grid, 256, 0, stream>>>(p, tpb);
-    else if (lanes <= 4) k_cache_append<T, 4><<<grid, 256, 0, stream>>>(p, tpb);
-    else if (lanes <= 8) k_cache_append<T, 8><<<grid, 256, 0, stream>>>(p, tpb);
+    if (lpr == 2) k_cache_append<T, 2><<<grid, 256, 0, stream>>>(p, tpb);
+    else if (lpr == 4) k_cache_append<T, 4><<<grid, 256, 0, stream>>>(p, tpb);
+    else if (lpr == 8) k_cache_append<T, 8><<<grid, 256, 0, stream>>>(p, tpb);
     else k_cache_append<T, 16><<<grid, 256, 0, stream>>>(p, tpb);
     return hipGetLastError();
 }
@@ -442,7 +450,7 @@ __global__ __launch_bounds__(256) void k_pages_apply(PagesProblem p, PagesWs w, 
 // instruction more in its loops is felt (16 cycles per 1024 threads): a wave walks rows,
 // not entries, and what a row says stays in scalars (entry by entry the reorder of 200 rows
 // took 22 us). Against the launches above, replayed from a graph: 200 rows of 123 entries,
-// 9015 pages, few copies 12.3 and 16.7 us; 64 rows of 39, 22 MB moved 11.8 and 18.6; a pool
+// 9015 pages, few copies 12.3 and 16.7 us; 64 rows of 39, 23 MB moved 11.8 and 18.6; a pool
 // of 101 pages squeezed 7.8 and 14.7, one of 2096 pages x 14 layers (909 MB moved) 191
 // (4.8 TB/s) and 201. At the limits, 16384 pages and 512 rows of 128: reorder 16.0 and 14.1,
 // compaction 18.8 and 21.5 (4 rows of 16384: 26.5 and 14.3, 29.9 and 21.3), but issuing from
