@@ -1,6 +1,18 @@
 // Attention of many new tokens over the paged cache (paged_attn_device.h says what a
 // workgroup computes): tiles of 128 query rows, 32 per wave, over shared chunks of 64
-// positions.
+// positions, the next chunk landing in LDS while this one is used.
+//
+// Bound: issue. A wave's chunk is 32 matrix products (1024 cycles of its SIMD's matrix unit)
+// and about 850 cycles of softmax on the vector unit, of which 512 are the exponentials;
+// two workgroups share a CU, and what overlaps is one's products with the other's softmax.
+// 2 x 2048 tokens of 28 heads, head size 128, over contexts of 8192: 429 us, 0.98 PFLOP/s (a
+// plain 8192^3 bf16 product reaches 1.21 here). What led there from 562: operands of both
+// products read ahead (541), a base that rarely moves (509), V rows swizzled for the
+// transposed reads (501), neighbouring tiles on one XCD (469; 490 on the card of the next figures), wave
+// priority to the products (475), no lane waiting for its row's other lane (443), row sums
+// by two-element dot products (436), V of a whole chunk read at once (429).
+// Not kept: the next chunk's scores beside this one's softmax within a wave (it spills at
+// two waves per SIMD, 1061; with one wave 628), in halves (559), priority by workgroup (447).
 #include "paged_attn_device.h"
 
 namespace mot {
@@ -117,6 +129,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
             // a chunk that no row of this wave sees adds nothing (uniform)
             if (wave_ok && kc <= wu1 && kc + 63 >= wlo) {
                 const bool masked = kc + 63 > wu0 || kc < wlo1 || kc < lo || kc + 64 > hi || ok != 15u;
+                __builtin_amdgcn_s_setprio(1);   // products first: the other workgroup's waves do softmax meanwhile
                 f32x16 sc[2];
                 u32x4 ka[2][D / 16];
 #pragma unroll
@@ -142,8 +155,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
                 uint32_t at[D / 32];
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db) at[db] = vat[db] + (uint32_t)st * (2 * KS * 16);
-                u32x2 va[D / 8];
+                u32x2 va[D / 8], vb[D / 8];
                 read_vt2<D, 0>(at, va);   // while the products run
+                read_vt2<D, 2 * 16 * D * 2>(at, vb);
+                __builtin_amdgcn_s_setprio(0);
                 if (masked) {
 #pragma unroll
                     for (int kb = 0; kb < 2; ++kb)
@@ -158,9 +173,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) cm = fmaxf(cm, sc[kb][e]);
-                cm = fmaxf(cm, __shfl_xor(cm, 32, 64));
-                const float top = cm * p.scale_log2;
-                if (__builtin_amdgcn_ballot_w64(top > mo + kSlack)) {
+                // no lane waits for its row's other lane (base and row sum): they meet where the
+                // base moves, and at the end
+                if (__builtin_amdgcn_ballot_w64(cm * p.scale_log2 > mo + kSlack)) {
+                    const float top = fmaxf(cm, __shfl_xor(cm, 32, 64)) * p.scale_log2;
                     const float mon = fmaxf(mo, top), alpha = __builtin_amdgcn_exp2f(mo - base_of(mon));
                     l *= alpha;
 #pragma unroll
@@ -170,33 +186,30 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
                     mo = mon;
                 }
                 const float off = base_of(mo);
-                float rs = 0.f;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float ex = __builtin_amdgcn_exp2f(fmaf(sc[kb][e], p.scale_log2, -off));
-                        sc[kb][e] = ex;
-                        rs += ex;
-                    }
-                rs += __shfl_xor(rs, 32, 64);
-                l += rs;
+                    for (int e = 0; e < 16; ++e) sc[kb][e] = __builtin_amdgcn_exp2f(fmaf(sc[kb][e], p.scale_log2, -off));
                 auto step = [&](int s, const u32x2* v) {
                     const int kb = s >> 1, e0 = 8 * (s & 1);
                     const u32x4 pf = {pack_bf16x2(sc[kb][e0], sc[kb][e0 + 1]), pack_bf16x2(sc[kb][e0 + 2], sc[kb][e0 + 3]),
                                       pack_bf16x2(sc[kb][e0 + 4], sc[kb][e0 + 5]), pack_bf16x2(sc[kb][e0 + 6], sc[kb][e0 + 7])};
 #pragma unroll
+                    for (int i = 0; i < 4; ++i) l = add_bf16x2(pf[i], l);
+#pragma unroll
                     for (int db = 0; db < D / 32; ++db)
                         acc[db] = mfma_32x32x16(u32x4{v[2 * db].x, v[2 * db].y, v[2 * db + 1].x, v[2 * db + 1].y}, pf, acc[db]);
                 };
+                __builtin_amdgcn_s_setprio(1);
                 step(0, va);
                 step(1, va + D / 16);
-                read_vt2<D, 2 * 16 * D * 2>(at, va);
-                step(2, va);
-                step(3, va + D / 16);
+                step(2, vb);
+                step(3, vb + D / 16);
+                __builtin_amdgcn_s_setprio(0);
             }
             barrier();   // the next chunk has landed; every wave is done with this one
         }
+        l += __shfl_xor(l, 32, 64);
         if (!exact) {
             float t = 0.f;   // NaN where an accumulator is not finite
 #pragma unroll

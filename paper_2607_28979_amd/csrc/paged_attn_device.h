@@ -164,6 +164,13 @@ constexpr uint32_t kPastEnd = 0x80000000u;   // byte offset that every group's b
 // those up to 1, and the accumulators are rarely rescaled.
 constexpr float kSlack = 8.f;
 
+// l + both bf16 of w: a row's sum takes the probabilities as they go into the product with V,
+// rounded, two in one instruction.
+__device__ __forceinline__ float add_bf16x2(uint32_t w, float l) {
+    typedef __bf16 two __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(two, w), __builtin_bit_cast(two, 0x3f803f80u), l, false);
+}
+
 // Running softmax of a row: `mo` is the largest exponent so far (base 2), -inf
 // before the first visible position; `base` replaces it where it is -inf.
 __device__ __forceinline__ float base_of(float mo) { return mo == -INFINITY ? 0.f : mo; }
