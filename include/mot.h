@@ -453,8 +453,9 @@ mot_status mot_backbone_translate(const void* src_k, const void* src_v, const in
  *                of the call among them (cut to 0 .. max_pages * page_size)
  *   new_start    device int32 [B + 1] or NULL: the new tokens of sequence b
  *                are the rows new_start[b] .. new_start[b + 1] - 1 of the
- *                call's row tensors (cut to 0 .. n_new).  NULL: every sequence
- *                has max_new of them, at batch row b
+ *                call's row tensors (cut to 0 .. n_new).  They ascend; where
+ *                they do not, what the outputs' new rows hold is unspecified.
+ *                NULL: every sequence has max_new of them, at batch row b
  *
  * New token i of the c of sequence b is at position kv_len[b] - c + i.  Rows
  * of no sequence are left as they are, and so are, of a sequence with more

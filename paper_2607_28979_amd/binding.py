@@ -628,8 +628,10 @@ def paged_attention(q, k_pages, v_pages, table, kv_len, o, new_start=None, max_n
         _refuse(2, "q must be [B][new][H_q][D] or [tokens][H_q][D]")
     lead, n_new, mx = c.new_rows(q, "q", new_start, max_new)
     H_q = q.shape[-2]
-    if scale is not None and not scale > 0:
-        _refuse(2, "scale must be positive")
+    if scale is not None and not 1.2e-38 <= scale <= 3.4e38:
+        _refuse(2, "scale must be a positive float32")
+    if not (0 <= window < 1 << 31 and 0 <= max_kv < 1 << 31):
+        _refuse(2, "window = %s and max_kv = %s must be in [0, 2^31)" % (window, max_kv))
     sizes = _ATTEND.pack(n_new, mx, H_q, window, max_kv, scale or 0.0, *c.rows(q, "q", lead, H_q), *c.rows(o, "o", lead, H_q))
     held, at, nbytes = None, 0, 0
     if scratch is not False:
@@ -662,6 +664,8 @@ def cache_append(q, k, v, q_out, k_pages, v_pages, table, kv_len, new_start=None
     if some.dim() < 3 + (c.L > 0):
         _refuse(2, "rows must be %s[B][new][heads][D] or packed" % ("[L]" if c.L else ""))
     lead, n_new, mx = c.new_rows(some, "q" if k is None else "k", new_start, max_new)
+    if not 0 <= eps <= 3.4e38:
+        _refuse(2, "eps must be >= 0 and finite")
     H_q = rot = 0
     qs = qos = ks = vs = _NO_STRIDES
     if q is not None:

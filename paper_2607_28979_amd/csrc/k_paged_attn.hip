@@ -19,8 +19,11 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendProblem p, int rows) {
     const Partial pt = partial_of(p, rows);
     const int2 span = pt.span[b * p.c.H_kv + kvh];
     const NewTokens nt = new_tokens(p.c, b);
-    if (t >= nt.n || span.y == 1) return;   // uniform over the workgroup
+    if (t >= nt.n) return;   // uniform over the workgroup
     const int r = t * G + h - kvh * G, tile = r / rows, tiles = div_up(nt.n * G, rows);
+    // whole ones are done (uniform); starts that do not ascend may make more tiles than there are workgroups, and spans that
+    // no one has left: nothing outside the partial tiles is read
+    if (span.x < 0 || span.y < 2 || span.x + (int64_t)span.y * tiles > 2 * p.n_split) return;
     const int64_t at = (int64_t)(span.x + tile) * pt.R + r - tile * rows, step = (int64_t)tiles * pt.R;
     float M = -INFINITY, l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};

@@ -279,6 +279,25 @@ def test_attention_of_many_sequences(B, t, new):
     assert (o[int(counts.sum()):] == KEEP).all()
 
 
+@pytest.mark.parametrize("t,n", [("bf16", 1), ("bf16", 60), ("f32", 9)])
+def test_attention_of_starts_that_do_not_ascend(t, n):
+    """Starts out of order name rows twice, more than the call has: the rows of no sequence
+    and the pools stay as they are, and the next call is right."""
+    import torch
+    rng = np.random.default_rng(n)
+    c = Cache(rng, [1500] * 40, 16, 2, 128, t, stale=False, max_pages=128)
+    q, _ = _rand(rng, (n + 2, 12, 128), t)
+    k, v = c.k.clone(), c.v.clone()
+    o = torch.full_like(q, KEEP)
+    start = [0, n] * 20 + [0]
+    print("case starts", t, n, flush=True)
+    mb.paged_attention(q, c.k, c.v, c.d_table, c.d_kv, o, new_start=_i32(start))
+    mb.paged_attention(q, c.k, c.v, c.d_table, c.d_kv, o, new_start=_i32([s - 5 for s in start[::-1]]))
+    torch.cuda.synchronize()
+    assert (o[n:] == KEEP).all() and torch.equal(k, c.k) and torch.equal(v, c.v)
+    _attend(c, q[:n], [0] * 39 + [n])
+
+
 def test_attention_repeats_itself_over_two_streams():
     """Calls on two streams at once, each with its own partial sums, give the bits of calls
     one after the other."""
@@ -738,7 +757,8 @@ def test_binding_refuses():
                    dict(k_pages=c.k.float()), dict(k_pages=c.k.half(), v_pages=c.v.half()), dict(v_pages=c.v[:-1]),
                    dict(k_pages=c.k.transpose(1, 2), v_pages=c.v.transpose(1, 2)), dict(table=c.d_table.long()),
                    dict(table=c.d_table[:, ::2]), dict(kv_len=c.d_kv[:1]), dict(kv_len=c.d_kv.cpu()), dict(max_new=2),
-                   dict(new_start=_i32([0, 3])), dict(scale=-1.0), dict(window=-1), dict(o=q), dict(q=q.transpose(2, 3)),
+                   dict(new_start=_i32([0, 3])), dict(scale=-1.0), dict(scale=1e-50), dict(scale=1e60), dict(window=-1),
+                   dict(window=1 << 31), dict(max_kv=1 << 40), dict(o=q), dict(q=q.transpose(2, 3)),
                    dict(o=o[:, :, :1].expand(2, 3, 4, 64)), dict(k_pages=c.k[None], v_pages=c.v[None]),
                    dict(scratch=torch.empty(64))):
         with pytest.raises(mb.MotError):
@@ -749,7 +769,7 @@ def test_binding_refuses():
     for change in (dict(q_out=None), dict(v=None), dict(k=None), dict(q=None, q_out=None, k=None, v=None), dict(k=q), dict(k=k[:, :2]),
                    dict(inv_freq=f.double()), dict(inv_freq=f[:4]), dict(inv_freq=torch.ones(64, device="cuda")), dict(inv_freq=f[:0]),
                    dict(q_gain=f.bfloat16()), dict(k_gain=torch.ones(64, device="cuda")), dict(positions=_i32([1, 2])),
-                   dict(eps=-1.0), dict(q_out=q.transpose(0, 1).contiguous().transpose(0, 1)[:, :, :2])):
+                   dict(eps=-1.0), dict(eps=1e60), dict(q_out=q.transpose(0, 1).contiguous().transpose(0, 1)[:, :, :2])):
         with pytest.raises(mb.MotError):
             mb.cache_append(**{**good, **change})
     new, one = torch.empty_like(c.d_table), _i32([0])
