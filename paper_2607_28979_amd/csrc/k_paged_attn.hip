@@ -8,7 +8,9 @@ namespace {
 
 // The partial sums of a cut (sequence, KV head), brought to one base and added, in the order
 // of the parts within each of the groups of D / 4 threads, then of the groups.  A
-// workgroup per query row.  grid (max_new * H_q, B); rows: of a tile
+// workgroup per query row, four parts' loads of every group under way together: it is all
+// latency (48 tokens of 28 heads over up to 8192 positions: 4.8 us; one token: 3.4).
+// grid (max_new * H_q, B); rows: of a tile
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_paged_join(AttendProblem p, int rows) {
     constexpr int TH = D / 4, NG = 256 / TH;   // threads of a group, groups

@@ -3,6 +3,10 @@
 // positions in turn, each with its own tiles and no barrier, and are joined through LDS at
 // the end.  On v_mfma_f32_16x16x4_f32: exact fp32 products, a quarter of the rate that
 // the bf16 products reach with a sixteenth of the work per instruction.
+//
+// Bound: latency for short contexts (3 x 64 tokens of 12 heads of 64 over 333 positions:
+// 9.5 us; tiles of 32 rows gave it too few workgroups, 24.7 us), issue of the fp32 products
+// for long ones (500 tokens of 12 heads of 128 over 2000: 96 us, 56 TFLOP/s).
 #include "paged_attn_device.h"
 
 namespace mot {
