@@ -98,10 +98,10 @@ int tile_rows(const AttendProblem& p, bool bf16) {
 // Few rows, calls back to back, whole against cut: one sequence of 500 positions 9.0 /
 // 12.6 us, 800 10.9 / 12.5, 1100 12.9 / 12.5, 1500 16.5 / 12.4; 32 of 1000 15.9 / 18.8; 48
 // of 205 to 8192 104 / 52 (kernels).  Tiles of 128 rows (kernels): 37 new tokens on 8000
-// 170 / 29 us, 200 on 1000 28.6 / 28.5, 2 x 300 on 700 22.6 / 47, 2 x 500 alone 20 / 54,
-// 16 x 20 on up to 6000 129 / 36, 1000 on 4000 95 / 103, 2 x 300 on 3000 with 16 heads
-// of 64 53 / 43.  fp32: 12 heads of 64, one token on 1000 19 / 10.6, 3 x 64 on 333 9.9 /
-// 12.8, 40 ragged ones on up to 2000 47 / 41; 12 heads on 2 of 128, 500 tokens on 2000 106 / 96.
+// 167 / 28 us, 200 on 1000 28.5 / 28.4, 2 x 300 on 700 23 / 47, 2 x 500 alone 20 / 57,
+// 16 x 20 on up to 6000 129 / 36, 1000 on 4000 91 / 120, 2 x 300 on 3000 with 16 heads
+// of 64 51 / 44.  fp32: 12 heads of 64, one token on 1000 19 / 10.2, 3 x 64 on 333 10 /
+// 16, 40 ragged ones on up to 2000 47 / 42; 12 heads on 2 of 128, 500 tokens on 2000 105 / 97.
 // Shares: 7/8 of the workgroups that the chip holds (two per CU at D = 128, three at 64),
 // since remainders add some: 30 ragged contexts on 2 heads 18.6 us with 448, 22.1
 // with 512 to 704.
