@@ -394,7 +394,8 @@ __device__ __forceinline__ void copy_item(const PagesProblem& p, int64_t it, int
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (x0 + i * THREADS < end) *reinterpret_cast<u32x4*>(to + off[i]) = v[i];
+            // past the caches: 23 MB of last pages 11.9 -> 10.7 us, 455 MB of pages 192 -> 189
+            if (x0 + i * THREADS < end) __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4*>(to + off[i]));
     }
 }
 __host__ __device__ inline int copy_pieces(const PagesProblem& p) {
@@ -450,8 +451,8 @@ __global__ __launch_bounds__(256) void k_pages_apply(PagesProblem p, PagesWs w, 
 // instruction more in its loops is felt (16 cycles per 1024 threads): a wave walks rows,
 // not entries, and what a row says stays in scalars (entry by entry the reorder of 200 rows
 // took 22 us). Against the launches above, replayed from a graph: 200 rows of 123 entries,
-// 9015 pages, few copies 12.3 and 16.7 us; 64 rows of 39, 23 MB moved 11.8 and 18.6; a pool
-// of 101 pages squeezed 7.8 and 14.7, one of 2096 pages x 14 layers (909 MB moved) 191
+// 9015 pages, few copies 12.3 and 16.7 us; 64 rows of 39, 23 MB moved 10.7 and 18.6; a pool
+// of 101 pages squeezed 7.8 and 14.7, one of 2096 pages x 14 layers (909 MB moved) 189
 // (4.8 TB/s) and 201. At the limits, 16384 pages and 512 rows of 128: reorder 16.0 and 14.1,
 // compaction 18.8 and 21.5 (4 rows of 16384: 26.5 and 14.3, 29.9 and 21.3), but issuing from
 // the host 7 and 16 us.
