@@ -24,13 +24,22 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
         for (int j = 0; j < 4; ++j) x[4 * i + j] = w[j];
     }
 }
-__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
-    *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                                         pack_bf16x2(x[6], x[7])};
+// PAST: past the caches
+template <bool PAST, typename V>
+__device__ __forceinline__ void store16(V* p, V v) {
+    if constexpr (PAST) __builtin_nontemporal_store(v, p);
+    else *p = v;
 }
+template <bool PAST>
+__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
+    store16<PAST>(reinterpret_cast<u32x4*>(p),
+            u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])});
+}
+template <bool PAST>
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) reinterpret_cast<f32x4*>(p)[i] = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+    for (int i = 0; i < 2; ++i)
+        store16<PAST>(reinterpret_cast<f32x4*>(p) + i, f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]});
 }
 
 constexpr int kMostTokens = 4;   // tokens of a workgroup
@@ -42,12 +51,12 @@ constexpr int kMostTokens = 4;   // tokens of a workgroup
 // token's heads: computed once per workgroup, into LDS; position * inv_freq in
 // fp64, since fp32 leaves an error of 2e-3 turns at position 32768.
 // Bound: bytes for long prompts (4096 tokens of 28 + 2 x 4 heads of 128, 75 MB: 17 us of
-// which 3.5 are the launch; 28 layers of 1501 tokens, 172 MB: 37 us, 4.7 TB/s), the launch
+// which 3.5 are the launch; 28 layers of 1501 tokens, 172 MB: 28 us, 6.1 TB/s), the launch
 // and one chain of loads for single tokens (32 sequences: 5 us).  Rows two at a time, for
 // more loads under way, took 108 registers and 10 to 25 % longer.
 //
 // grid (ceil(max_new / tpb), B, L), 256 threads
-template <typename T, int LPR>
+template <typename T, int LPR, bool PAST>
 __global__ __launch_bounds__(256) void k_cache_append(AppendProblem p, int tpb) {
     __shared__ float2 s_turn[kMostTokens][128];
     __shared__ int64_t s_slot[kMostTokens];   // element offset of the token's place, -1: not stored
@@ -145,10 +154,18 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendProblem p, int tpb) 
             }
         }
         if (live) {
-            store8(dst + 8 * lo, x);
-            store8(dst + 8 * hi, y);
+            store8<PAST>(dst + 8 * lo, x);
+            store8<PAST>(dst + 8 * hi, y);
         }
     }
+}
+
+template <typename T, bool PAST>
+void append_by(const AppendProblem& p, int lpr, int tpb, dim3 grid, hipStream_t stream) {
+    if (lpr == 2) k_cache_append<T, 2, PAST><<<grid, 256, 0, stream>>>(p, tpb);
+    else if (lpr == 4) k_cache_append<T, 4, PAST><<<grid, 256, 0, stream>>>(p, tpb);
+    else if (lpr == 8) k_cache_append<T, 8, PAST><<<grid, 256, 0, stream>>>(p, tpb);
+    else k_cache_append<T, 16, PAST><<<grid, 256, 0, stream>>>(p, tpb);
 }
 
 template <typename T>
@@ -156,16 +173,20 @@ hipError_t append_as(const AppendProblem& p, hipStream_t stream) {
     // Tokens of a workgroup: one until there are several for every CU, then four where four
     // tokens' heads are one turn of its threads, else two.  Measured (us with 1, 2, 4 tokens,
     // heads of 128): 36 heads, 512 tokens 5.4, 6.2, 7.8; 2048: 11.8, 11.1, 12.2; 8192: 38,
-    // 37, 42; 8 heads, 1800 tokens 4.6, 4.2, 4.1; 42000: 51, 42, 37 (8 tokens: 39).
+    // 37, 42; 8 heads, 1800 tokens 4.6, 4.2, 4.1; 42000: 51, 42, 37 (8 tokens: 39), all with
+    // ordinary stores.
     const int64_t tokens = (int64_t)p.c.max_new * p.c.B * p.L;
     const int lanes = p.c.D >> 4, lpr = lanes <= 2 ? 2 : lanes <= 4 ? 4 : lanes <= 8 ? 8 : 16;
     const int heads = (p.q ? p.H_q : 0) + (p.k ? 2 * p.c.H_kv : 0);
     const int tpb = tokens < 1792 ? 1 : kMostTokens * heads * lpr <= 256 ? kMostTokens : 2;
     const dim3 grid((p.c.max_new + tpb - 1) / tpb, p.c.B, p.L);
-    if (lpr == 2) k_cache_append<T, 2><<<grid, 256, 0, stream>>>(p, tpb);
-    else if (lpr == 4) k_cache_append<T, 4><<<grid, 256, 0, stream>>>(p, tpb);
-    else if (lpr == 8) k_cache_append<T, 8><<<grid, 256, 0, stream>>>(p, tpb);
-    else k_cache_append<T, 16><<<grid, 256, 0, stream>>>(p, tpb);
+    // Stores past the caches where what is written is more than attention finds there again:
+    // 28 layers of 1501 tokens, 86 MB written, 36.6 -> 28.4 us, 8192 tokens of 36 heads, 75 MB,
+    // 36.7 -> 26.7.  Below, the call itself gains little (38 MB 17.5 -> 16.8) and attention
+    // after it loses more (4096 tokens, both calls 202 -> 205).
+    const bool past = (int64_t)p.c.n_new * p.L * heads * p.c.D * (int64_t)sizeof(T) > 64 << 20;
+    if (past) append_by<T, true>(p, lpr, tpb, grid, stream);
+    else append_by<T, false>(p, lpr, tpb, grid, stream);
     return hipGetLastError();
 }
 

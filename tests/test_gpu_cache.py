@@ -453,6 +453,34 @@ def test_append(case):
     _check_append(case, *a, before)
 
 
+@pytest.mark.parametrize("t,L,D,n,ps", [("bf16", 1, 128, 8192, 64), ("f32", 1, 64, 8200, 16), ("bf16", 3, 32, 13000, 16)])
+def test_append_of_many_equals_parts(t, L, D, n, ps):
+    """A call that writes more than the caches hold, and the same tokens in parts: the same
+    bits, in both of which every row is written once."""
+    import torch
+    Hq, H = 28, 4
+    g = torch.Generator(device="cuda").manual_seed(n)
+    lead = () if L == 1 else (L,)
+    x = torch.randn(lead + (1, n, Hq + 2 * H, D), generator=g, device="cuda").to(_dt(t))
+    f = torch.rand(D // 2, generator=g, device="cuda")
+    gain = (1 + 0.1 * torch.randn((L, D), generator=g, device="cuda")).to(_dt(t))
+    pages = -(-n // ps)
+    table = torch.randperm(pages + 2, generator=g, device="cuda").int()[:pages][None].contiguous()
+    assert n * L * (Hq + 2 * H) * D * x.element_size() > 64 << 20
+    out = []
+    for part in (n, 1025):
+        k, v = (torch.full(lead + (pages + 2, ps, H, D), KEEP, device="cuda", dtype=_dt(t)) for _ in range(2))
+        qo = torch.full(lead + (1, n, Hq, D), KEEP, device="cuda", dtype=_dt(t))
+        for at in range(0, n, part):
+            m = slice(at, min(at + part, n))
+            y = x[..., m, :, :]
+            mb.cache_append(y[..., :Hq, :], y[..., Hq:Hq + H, :], y[..., Hq + H:, :], qo[..., m, :, :], k, v, table, _i32([m.stop]),
+                            inv_freq=f, q_gain=gain, k_gain=gain)
+        out.append((k, v, qo))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+    assert int((out[0][1] == KEEP).all(-1).all(-1).sum()) == L * ((pages + 2) * ps - n)
+
+
 def test_append_far_positions_and_given_ones():
     """Angles of positions near 2^20 from the places, and of given positions (the
     places then at the sequence's end, as ever)."""
