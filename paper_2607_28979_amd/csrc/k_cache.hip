@@ -51,7 +51,7 @@ constexpr int kMostTokens = 4;   // tokens of a workgroup
 // token's heads: computed once per workgroup, into LDS; position * inv_freq in
 // fp64, since fp32 leaves an error of 2e-3 turns at position 32768.
 // Bound: bytes for long prompts (4096 tokens of 28 + 2 x 4 heads of 128, 75 MB: 17 us of
-// which 3.5 are the launch; 28 layers of 1501 tokens, 172 MB: 28 us, 6.1 TB/s), the launch
+// which 3.5 are the launch; 28 layers of 1501 tokens, 172 MB: 28 to 32 us), the launch
 // and one chain of loads for single tokens (32 sequences: 5 us).  Rows two at a time, for
 // more loads under way, took 108 registers and 10 to 25 % longer.
 //
