@@ -773,6 +773,47 @@ def test_graph_of_a_decoding_step():
         assert all(torch.equal(p, w) for p, w in zip(pools, twin)), i
 
 
+def test_graph_of_a_large_pool():
+    """Reordering and compaction of a pool too large for one launch, captured with a workspace
+    of the graph's own and replayed with new rows, other work between."""
+    import torch
+    rng = np.random.default_rng(8)
+    B, M, n_pages = 30, 20, 20000
+    c = Cache(rng, rng.integers(0, M * 16 + 1, B).tolist(), 16, 1, 16, "bf16", L=1, stale=False, max_pages=M, spare=n_pages)
+    assert mb.cache_workspace_bytes(c.k, c.v, c.d_table, B) > 0
+    pools, first = (c.k, c.v), (c.k.clone(), c.v.clone())
+    src, keep, want = (_i32(np.zeros(B)) for _ in range(3))
+    out = [torch.empty_like(c.d_table) for _ in range(2)] + [_i32([0]), _i32([0])]
+
+    def step(new, packed, missing, used):
+        mb.cache_reorder(*pools, c.d_table, src, keep, want, new, missing)
+        mb.cache_compact(*pools, new, packed, used)
+
+    step(*out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(*out)
+    for i in range(4):
+        s = rng.integers(-1, B, B)
+        k = np.where(s >= 0, np.minimum(np.array(c.kv)[s], rng.integers(0, M * 16 + 1, B)), 0)
+        src.copy_(_i32(s)), keep.copy_(_i32(k)), want.copy_(_i32(k + rng.integers(0, 40, B)))
+        got = []
+        for run in (graph.replay, lambda: step(*out)):
+            for p, f in zip(pools, first):
+                p.copy_(f)
+            for x in out:
+                x.fill_(-7)
+            run()
+            torch.cuda.synchronize()
+            (torch.randn(500, 500, device="cuda") @ torch.randn(500, 500, device="cuda")).sum().item()
+            got.append([x.clone() for x in (*out, *pools)])
+        assert all(torch.equal(a, b) for a, b in zip(*got)), i
+        wk, wv, wt, wm = ref.cache_reorder(_np(first[0]), _np(first[1]), c.table, _np(src).astype(int), _np(keep).astype(int), _np(want).astype(int))
+        wk, wv, wp, wn = ref.cache_compact(wk, wv, wt)
+        assert np.array_equal(out[0].cpu().numpy(), wt) and np.array_equal(out[1].cpu().numpy(), wp)
+        assert int(out[2]) == wm and int(out[3]) == wn and np.array_equal(_np(c.k), wk) and np.array_equal(_np(c.v), wv)
+
+
 def test_binding_refuses():
     """What the binding sees in the tensors: types, devices, shapes, strides."""
     import torch
