@@ -503,8 +503,8 @@ typedef struct {
  *                pitch and all); o must not overlap q, the pools or the tables
  *   n_new        rows of q and o over all sequences (B * max_new without
  *                new_start)
- *   max_new      most new tokens of a sequence (the tiles are chosen by it: a close
- *                bound for single tokens packed by new_start)
+ *   max_new      most new tokens of a sequence (packed: n_new will do, a close
+ *                bound is a little faster)
  *   H_q          query heads, a multiple of H_kv
  *   window       0: every position up to u; else that many, u among them
  *   max_kv       0, or a bound on kv_len that is better than max_pages *

@@ -613,8 +613,7 @@ def paged_attention(q, k_pages, v_pages, table, kv_len, o, new_start=None, max_n
     q, o: [B][new][H_q][D], or with new_start (int32 [B + 1]) packed
     [tokens][H_q][D]; any strides with contiguous heads.  kv_len int32 [B] counts
     the new tokens, max_new (packed; default: all rows) bounds those of a
-    sequence and chooses the tiles (give 1 for packed single tokens).  window 0: all
-    positions up to the token's.
+    sequence.  window 0: all positions up to the token's.
 
     ``scratch``: memory for calls that cut long sequences.  None: taken from
     torch's allocator for this call (none under a capture begun outside torch).

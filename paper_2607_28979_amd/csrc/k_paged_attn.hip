@@ -10,13 +10,29 @@ namespace {
 // of the parts within each of the groups of D / 4 threads, then of the groups.  A
 // workgroup per query row, four parts' loads of every group under way together: it is all
 // latency (48 tokens of 28 heads over up to 8192 positions: 4.8 us; one token: 3.4).
-// grid (max_new * H_q, B); rows: of a tile
+// grid (max_new * H_q, B), or by_row (n_new * H_q) of packed tokens, whose sequence every
+// wave finds among the starts; rows: of a tile
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_paged_join(AttendProblem p, int rows) {
+__global__ __launch_bounds__(256) void k_paged_join(AttendProblem p, int rows, bool by_row) {
     constexpr int TH = D / 4, NG = 256 / TH;   // threads of a group, groups
     __shared__ f32x4 s_acc[256];
     __shared__ float2 s_ml[NG];
-    const int b = blockIdx.y, t = blockIdx.x / p.H_q, h = blockIdx.x - t * p.H_q, G = p.H_q / p.c.H_kv, kvh = h / G;
+    const int G = p.H_q / p.c.H_kv, h = blockIdx.x % p.H_q, kvh = h / G;
+    int b = blockIdx.y, t = blockIdx.x / p.H_q;
+    if (by_row) {
+        const int lane = threadIdx.x & 63, row = t;
+        b = -1;
+        for (int b0 = 0; b0 < p.c.B && b < 0; b0 += 64) {
+            const NewTokens nt = new_tokens(p.c, min(b0 + lane, p.c.B - 1));
+            const unsigned long long here = __builtin_amdgcn_ballot_w64(b0 + lane < p.c.B && row >= nt.row && row < nt.row + nt.n);
+            if (here) {
+                const int who = __builtin_ctzll(here);
+                b = b0 + who;
+                t = row - __builtin_amdgcn_readlane(nt.row, who);
+            }
+        }
+        if (b < 0) return;   // uniform over the workgroup
+    }
     const int c = threadIdx.x % TH, grp = threadIdx.x / TH;
     const Partial pt = partial_of(p, rows);
     const int2 span = pt.span[b * p.c.H_kv + kvh];
@@ -85,9 +101,13 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendProblem p, int rows) {
         *reinterpret_cast<f32x4*>(o) = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
 }
 
-// Rows of a tile: 32 where all of a sequence's fit, else 128; fp32 16.
+// Rows of a tile: 32 where all of a sequence's fit, or an average one's do (packed tokens
+// with a loose max_new), else 128; fp32 16.  With no max_new, 128 and 32 rows: 48 single
+// tokens on 4000 114 and 86 us, 256 on 300 66 and 42, 32 x 4 on 2000 118 and 41, 47 and 100 of
+// one sequence on 4000 116 and 102.
 int tile_rows(const AttendProblem& p, bool bf16) {
-    return !bf16 ? 16 : (int64_t)p.c.max_new * (p.H_q / p.c.H_kv) <= 32 ? 32 : 128;
+    const int64_t G = p.H_q / p.c.H_kv;
+    return !bf16 ? 16 : p.c.max_new * G <= 32 || (p.c.n_new * G <= 32 * p.c.B && p.c.B <= kMostSeq) ? 32 : 128;
 }
 
 }  // namespace
@@ -125,11 +145,12 @@ hipError_t launch_paged_attention(const AttendProblem& p, bool bf16, hipStream_t
     const int rows = tile_rows(p, bf16);
     hipError_t e = rows == 32 ? launch_paged_decode(p, stream) : bf16 ? launch_paged_chunk(p, stream) : launch_paged_f32(p, stream);
     if (e != hipSuccess || !p.part) return e;
-    const dim3 join(p.c.max_new * p.H_q, p.c.B);
-    if (bf16 && p.c.D == 128) k_paged_join<uint16_t, 128><<<join, 256, 0, stream>>>(p, rows);
-    else if (bf16) k_paged_join<uint16_t, 64><<<join, 256, 0, stream>>>(p, rows);
-    else if (p.c.D == 128) k_paged_join<float, 128><<<join, 256, 0, stream>>>(p, rows);
-    else k_paged_join<float, 64><<<join, 256, 0, stream>>>(p, rows);
+    const bool by_row = p.c.start && (int64_t)p.c.max_new * p.c.B > 2 * (int64_t)p.c.n_new;
+    const dim3 join((by_row ? p.c.n_new : p.c.max_new) * p.H_q, by_row ? 1 : p.c.B);
+    if (bf16 && p.c.D == 128) k_paged_join<uint16_t, 128><<<join, 256, 0, stream>>>(p, rows, by_row);
+    else if (bf16) k_paged_join<uint16_t, 64><<<join, 256, 0, stream>>>(p, rows, by_row);
+    else if (p.c.D == 128) k_paged_join<float, 128><<<join, 256, 0, stream>>>(p, rows, by_row);
+    else k_paged_join<float, 64><<<join, 256, 0, stream>>>(p, rows, by_row);
     return hipGetLastError();
 }
 

@@ -1,5 +1,6 @@
-// Attention of few new tokens (decoding) over the paged cache: a sequence's rows of one
-// KV head all fit a tile of 32 (paged_attn_device.h says what a workgroup computes).
+// Attention of few new tokens (decoding) over the paged cache: tiles of 32 rows, which
+// hold all rows of one KV head of most sequences (paged_attn_device.h says what a workgroup
+// computes).
 //
 // The waves of a workgroup take blocks of 32 positions in turn, each with its own
 // tiles and no barrier, and are joined through LDS at the end: K of the next block lands
@@ -19,7 +20,7 @@ namespace mot {
 namespace {
 
 // NW waves.  N: sequences per lane of the shared work (grid most_workgroups), 0: nothing
-// shared (grid B * H_kv)
+// shared, and a tile to a sequence (grid B * H_kv)
 template <int D, int NW, int N>
 __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
     constexpr int DC = D / 8, TILE = 32 * DC;        // 16-byte chunks of a row, of 32 rows
@@ -61,11 +62,11 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) vat[db] = lds_address(Vt + vrow * DC + ((4 * db + vch) ^ vswz(vrow))) + 8 * (l16 & 1);
 
-    const Tile tl = tile_of(p, nt, 0, 32);
+    const Tile tl = tile_of(p, nt, N > 0 ? wk.tile : 0, 32);
     const bool cut = wk.parts > 1;
     // this lane's query row
-    const bool row_ok = l32 < tl.n_rows;
-    const int rq = min(l32, tl.n_rows - 1), tok = rq / G, head = kvh * G + rq - tok * G;
+    const bool row_ok = tl.r0 + l32 < tl.n_rows;
+    const int rq = min(tl.r0 + l32, tl.n_rows - 1), tok = rq / G, head = kvh * G + rq - tok * G;
     u32x4 qop[D / 16];
     {
         const u32x4 zero = {0u, 0u, 0u, 0u};
@@ -74,12 +75,13 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
         for (int ks = 0; ks < D / 16; ++ks) qop[ks] = row_ok ? *reinterpret_cast<const u32x4*>(row + 16 * ks) : zero;
     }
     const int u = tl.u0 + tok, ulo = low_of(p, u);
-    const bool one = tl.t1 == 0;
+    const int tokens = tl.t1 - tl.t0 + 1;
+    const bool one = tokens == 1;
 
     // pass 0: all tokens; later passes, where that was not finite: one token each
-    for (int pass = one ? 1 : 0; pass <= tl.t1 + 1; ++pass) {
-        const int only = one ? 0 : pass - 1;      // token of this pass, -1: all
-        const bool exact = only >= 0;             // positions below `lo` read as zeros
+    for (int pass = one ? 1 : 0; pass <= tokens; ++pass) {
+        const int only = tl.t0 + pass - 1;        // token of an exact pass
+        const bool exact = pass > 0;              // positions below `lo` read as zeros
         const int lo = max(exact ? low_of(p, tl.u0 + only) : tl.lo, wk.lo);
         const int hi = min(exact ? max(tl.u0 + only + 1, 0) : tl.hi, wk.hi);
         f32x16 acc[D / 32];
@@ -136,7 +138,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
                 load_k(nx);
             }
             // rows that see every position of the block need no mask
-            if (kb < lo || kb + 31 > tl.u0 + (exact ? only : 0) || okb != 3u || p.window > 0) {
+            if (kb < lo || kb + 31 > tl.u0 + (exact ? only : tl.t0) || okb != 3u || p.window > 0) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int v = kb + 8 * (e >> 2) + 4 * g + (e & 3);
@@ -219,8 +221,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) t = fmaf(o4[c][j], 0.f, t);
         }
-        const int rt = r / G;
-        const bool store = r < tl.n_rows && (!exact || rt == only);
+        const int rr = tl.r0 + r, rt = rr / G;
+        const bool store = rr < tl.n_rows && (!exact || rt == only);
         if (!exact) {
             if (store && t != t) *s_bad = 1;
             __syncthreads();
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
             if (bad) continue;
         }
         if (store) {
-            const int hh = kvh * G + r - rt * G;
+            const int hh = kvh * G + rr - rt * G;
             if (cut) {
                 const Partial pt = partial_of(p, 32);
                 const int64_t row = partial_row(pt, wk) + r;
@@ -254,10 +256,13 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
 template <int D>
 hipError_t launch_d(const AttendProblem& p, hipStream_t stream) {
     const int whole = p.c.B * p.c.H_kv;
-    if (p.part) {
-        const unsigned grid = (unsigned)most_workgroups(p, 32);
-        if (p.c.B <= 64) k_paged_decode<D, 4, 1><<<grid, 256, 0, stream>>>(p);
-        else k_paged_decode<D, 4, kSeqPerLane><<<grid, 256, 0, stream>>>(p);
+    if (p.part || (int64_t)p.c.max_new * (p.H_q / p.c.H_kv) > 32) {
+        const AttendProblem s = shared_out(p);
+        const int64_t grid = most_workgroups(s, 32);
+        if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+        if (p.c.B <= 64 && !p.part && grid <= 256) k_paged_decode<D, 8, 1><<<(unsigned)grid, 512, 0, stream>>>(s);
+        else if (p.c.B <= 64) k_paged_decode<D, 4, 1><<<(unsigned)grid, 256, 0, stream>>>(s);
+        else k_paged_decode<D, 4, kSeqPerLane><<<(unsigned)grid, 256, 0, stream>>>(s);
     } else if (whole <= 256) {   // a CU for each: more waves
         k_paged_decode<D, 8, 0><<<whole, 512, 0, stream>>>(p);
     } else {

@@ -246,11 +246,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_f32(AttendProblem p, int tiles
 template <int D>
 hipError_t launch_d(const AttendProblem& p, hipStream_t stream) {
     const int tiles = div_up(p.c.max_new * (p.H_q / p.c.H_kv), 16);
-    const int64_t grid = p.part ? (most_workgroups(p, 16) + 7) / 8 * 8 : ((int64_t)p.c.B * p.c.H_kv * tiles + 7) / 8 * 8;
+    const bool own = !p.part && !scattered(p, 16, tiles);
+    const AttendProblem s = shared_out(p);
+    const int64_t grid = ((own ? (int64_t)p.c.B * p.c.H_kv * tiles : most_workgroups(s, 16)) + 7) / 8 * 8;
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-    if (!p.part) k_paged_f32<D, 0><<<(unsigned)grid, 256, 0, stream>>>(p, tiles);
-    else if (p.c.B <= 64) k_paged_f32<D, 1><<<(unsigned)grid, 256, 0, stream>>>(p, tiles);
-    else k_paged_f32<D, kSeqPerLane><<<(unsigned)grid, 256, 0, stream>>>(p, tiles);
+    if (own) k_paged_f32<D, 0><<<(unsigned)grid, 256, 0, stream>>>(p, tiles);
+    else if (p.c.B <= 64) k_paged_f32<D, 1><<<(unsigned)grid, 256, 0, stream>>>(s, tiles);
+    else k_paged_f32<D, kSeqPerLane><<<(unsigned)grid, 256, 0, stream>>>(s, tiles);
     return hipGetLastError();
 }
 
