@@ -44,6 +44,23 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
 
 constexpr int kMostTokens = 4;   // tokens of a workgroup
 
+// The sequence whose new tokens packed row `row` is among (-1: none), and its number among
+// them, by a wave: the last sequence that starts at `row` or before, 64 starts at a time.
+__device__ __forceinline__ int sequence_of(const PageTable& c, int row, int* i) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = c.B;   // it is one of lo .. lo + n - 1
+    while (n > 1) {
+        const int step = (n + 63) / 64, at = lo + lane * step;
+        const unsigned long long before = __builtin_amdgcn_ballot_w64(lane * step < n && c.start[min(at, c.B - 1)] <= row);
+        const int k = before ? 63 - __builtin_clzll(before) : 0;
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    const NewTokens t = new_tokens(c, lo);
+    *i = row - t.row;
+    return *i >= 0 && *i < t.n ? lo : -1;
+}
+
 // Norms, rotation and stores of `tpb` new tokens of one sequence and layer: rows are
 // the token's query, key and value heads, LPR lanes each, two 16-byte chunks of
 // 8 elements (bf16) per lane: c and c + rot / 16 of the rotated part, so that
@@ -55,21 +72,45 @@ constexpr int kMostTokens = 4;   // tokens of a workgroup
 // and one chain of loads for single tokens (32 sequences: 5 us).  Rows two at a time, for
 // more loads under way, took 108 registers and 10 to 25 % longer.
 //
-// grid (ceil(max_new / tpb), B, L), 256 threads
-template <typename T, int LPR, bool PAST>
+// grid (ceil(max_new / tpb), B, L), or FIND: (ceil(n_new / tpb), 1, L) over packed rows, whose
+// sequences it finds among the starts; 256 threads
+template <typename T, int LPR, bool PAST, bool FIND>
 __global__ __launch_bounds__(256) void k_cache_append(AppendProblem p, int tpb) {
     __shared__ float2 s_turn[kMostTokens][128];
     __shared__ int64_t s_slot[kMostTokens];   // element offset of the token's place, -1: not stored
-    const int b = blockIdx.y, l = blockIdx.z, tid = threadIdx.x, D = p.c.D;
-    const NewTokens nt = new_tokens(p.c, b);
-    const int i0 = blockIdx.x * tpb, m = min(tpb, nt.n - i0);
-    if (m <= 0) return;   // uniform over the workgroup
+    __shared__ int s_pos[kMostTokens], s_b[kMostTokens];   // its position, its sequence (FIND; -1: none)
+    const int l = blockIdx.z, tid = threadIdx.x, D = p.c.D, i0 = blockIdx.x * tpb;
+    const int b = FIND ? 0 : blockIdx.y;
+    NewTokens nt = {};
+    int m;
+    if constexpr (FIND) {
+        m = min(tpb, p.c.n_new - i0);
+        const int w = tid >> 6;
+        if (w < m) {
+            int i;
+            const int at = sequence_of(p.c, i0 + w, &i);
+            if ((tid & 63) == 0) {
+                s_b[w] = at;
+                const NewTokens n = new_tokens(p.c, max(at, 0));
+                s_pos[w] = n.kv - n.count + i;
+            }
+        }
+        __syncthreads();
+    } else {
+        nt = new_tokens(p.c, b);
+        m = min(tpb, nt.n - i0);
+        if (m <= 0) return;   // uniform over the workgroup
+    }
     const int pos0 = nt.kv - nt.count + i0;
+    auto position = [&](int t) { return FIND ? s_pos[t] : pos0 + t; };
+    auto offset = [&](const RowStrides& st, int t) {
+        return FIND ? (int64_t)(i0 + t) * st.token : row_offset(p.c, st, nt, b, i0 + t);
+    };
     if (tid < m) {
-        const int pos = pos0 + tid;
+        const int pos = position(tid), row = FIND ? s_b[tid] : b;
         int64_t at = -1;
-        if (pos >= 0) {
-            const int page = p.c.table[(int64_t)b * p.c.max_pages + (pos >> p.c.page_shift)];
+        if (pos >= 0 && row >= 0) {
+            const int page = p.c.table[(int64_t)row * p.c.max_pages + (pos >> p.c.page_shift)];
             if (page >= 0 && page < p.c.n_pages)
                 at = ((int64_t)l * p.c.n_pages + page) * p.c.page_elems +
                      (int64_t)(pos & ((1 << p.c.page_shift) - 1)) * p.c.ts;
@@ -80,7 +121,7 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendProblem p, int tpb) 
     if (p.inv_freq)
         for (int x = tid; x < m * half; x += 256) {
             const int t = x / half, r = x - t * half;
-            const int pos = p.positions ? p.positions[p.c.start ? nt.row + i0 + t : b * p.c.max_new + i0 + t] : pos0 + t;
+            const int pos = p.positions ? p.positions[p.c.start ? nt.row + i0 + t : b * p.c.max_new + i0 + t] : position(t);
             double turns = (double)pos * (double)p.inv_freq[r] * 0.15915494309189533577;
             turns -= rint(turns);
             float sn, cs;
@@ -94,13 +135,14 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendProblem p, int tpb) 
     const int lo = turned ? c : rc + c, hi = turned ? c + rc : lo + lanes - rc;   // chunks of 8
     for (int r = tid / LPR; r < m * heads; r += 256 / LPR) {
         const int t = r / heads, h = r - t * heads;
+        if (FIND && s_b[t] < 0) continue;   // a row of no sequence
         const int kind = h < nq ? 0 : h < nq + nk ? 1 : 2, hh = kind == 0 ? h : kind == 1 ? h - nq : h - nq - nk;
         const RowStrides& st = kind == 0 ? p.qs : kind == 1 ? p.ks : p.vs;
         const T* src = reinterpret_cast<const T*>(kind == 0 ? p.q : kind == 1 ? p.k : p.v) + l * st.layer +
-                       row_offset(p.c, st, nt, b, i0 + t) + hh * st.head;
+                       offset(st, t) + hh * st.head;
         T* dst;
         if (kind == 0) {
-            dst = reinterpret_cast<T*>(p.q_out) + l * p.qos.layer + row_offset(p.c, p.qos, nt, b, i0 + t) + hh * p.qos.head;
+            dst = reinterpret_cast<T*>(p.q_out) + l * p.qos.layer + offset(p.qos, t) + hh * p.qos.head;
         } else {
             const int64_t at = s_slot[t];
             if (at < 0) continue;   // uniform over the row's lanes
@@ -160,12 +202,12 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendProblem p, int tpb) 
     }
 }
 
-template <typename T, bool PAST>
+template <typename T, bool PAST, bool FIND>
 void append_by(const AppendProblem& p, int lpr, int tpb, dim3 grid, hipStream_t stream) {
-    if (lpr == 2) k_cache_append<T, 2, PAST><<<grid, 256, 0, stream>>>(p, tpb);
-    else if (lpr == 4) k_cache_append<T, 4, PAST><<<grid, 256, 0, stream>>>(p, tpb);
-    else if (lpr == 8) k_cache_append<T, 8, PAST><<<grid, 256, 0, stream>>>(p, tpb);
-    else k_cache_append<T, 16, PAST><<<grid, 256, 0, stream>>>(p, tpb);
+    if (lpr == 2) k_cache_append<T, 2, PAST, FIND><<<grid, 256, 0, stream>>>(p, tpb);
+    else if (lpr == 4) k_cache_append<T, 4, PAST, FIND><<<grid, 256, 0, stream>>>(p, tpb);
+    else if (lpr == 8) k_cache_append<T, 8, PAST, FIND><<<grid, 256, 0, stream>>>(p, tpb);
+    else k_cache_append<T, 16, PAST, FIND><<<grid, 256, 0, stream>>>(p, tpb);
 }
 
 template <typename T>
@@ -175,18 +217,24 @@ hipError_t append_as(const AppendProblem& p, hipStream_t stream) {
     // heads of 128): 36 heads, 512 tokens 5.4, 6.2, 7.8; 2048: 11.8, 11.1, 12.2; 8192: 38,
     // 37, 42; 8 heads, 1800 tokens 4.6, 4.2, 4.1; 42000: 51, 42, 37 (8 tokens: 39), all with
     // ordinary stores.
-    const int64_t tokens = (int64_t)p.c.max_new * p.c.B * p.L;
+    const int64_t tokens = (int64_t)p.c.n_new * p.L;
     const int lanes = p.c.D >> 4, lpr = lanes <= 2 ? 2 : lanes <= 4 ? 4 : lanes <= 8 ? 8 : 16;
     const int heads = (p.q ? p.H_q : 0) + (p.k ? 2 * p.c.H_kv : 0);
     const int tpb = tokens < 1792 ? 1 : kMostTokens * heads * lpr <= 256 ? kMostTokens : 2;
-    const dim3 grid((p.c.max_new + tpb - 1) / tpb, p.c.B, p.L);
+    // Packed rows one by one where most of the places that max_new admits are none: 200 single
+    // tokens and 1500 of one sequence, 36 heads of 128, 49 -> 9.5 us, 47 and 512 11.8 -> 5.7,
+    // 256 single ones with no bound 27 -> 5.2 (4.6 with it: finding the sequence).
+    const bool find = p.c.start && (int64_t)p.c.max_new * p.c.B > 2 * (int64_t)p.c.n_new;
+    const dim3 grid(((find ? p.c.n_new : p.c.max_new) + tpb - 1) / tpb, find ? 1 : p.c.B, p.L);
     // Stores past the caches where what is written is more than attention finds there again:
     // 28 layers of 1501 tokens, 86 MB written, 36.6 -> 28.4 us, 8192 tokens of 36 heads, 75 MB,
     // 36.7 -> 26.7.  Below, the call itself gains little (38 MB 17.5 -> 16.8) and attention
     // after it loses more (4096 tokens, both calls 202 -> 205).
     const bool past = (int64_t)p.c.n_new * p.L * heads * p.c.D * (int64_t)sizeof(T) > 64 << 20;
-    if (past) append_by<T, true>(p, lpr, tpb, grid, stream);
-    else append_by<T, false>(p, lpr, tpb, grid, stream);
+    if (past && find) append_by<T, true, true>(p, lpr, tpb, grid, stream);
+    else if (past) append_by<T, true, false>(p, lpr, tpb, grid, stream);
+    else if (find) append_by<T, false, true>(p, lpr, tpb, grid, stream);
+    else append_by<T, false, false>(p, lpr, tpb, grid, stream);
     return hipGetLastError();
 }
 

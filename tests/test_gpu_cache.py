@@ -502,6 +502,40 @@ def test_append_of_many_equals_parts(t, L, D, n, ps):
     assert int((out[0][1] == KEEP).all(-1).all(-1).sum()) == L * ((pages + 2) * ps - n)
 
 
+@pytest.mark.parametrize("B,most,L,t", [(3, 40, 1, "bf16"), (64, 9, 2, "bf16"), (65, 300, 1, "f32"), (700, 5, 1, "bf16"), (5000, 700, 1, "bf16")])
+def test_append_of_packed_tokens_without_a_bound(B, most, L, t):
+    """Packed tokens and no max_new, whose sequences are found row by row, give the bits of
+    the call with the bound: sequences of none, rows before the first and behind the last,
+    holes, given positions."""
+    import torch
+    rng = np.random.default_rng(B)
+    counts = rng.integers(0, 2, B)
+    counts[[0, B - 1]] = 1, 0
+    counts[2 * B // 3] = most
+    start = 2 + np.concatenate([[0], np.cumsum(counts)])
+    kv = counts + rng.integers(-1, 30, B)
+    c = Cache(rng, np.maximum(kv, 0).tolist(), 16, 2, 32, t, L=L, stale=False)
+    c.table[rng.integers(0, B, 2), 0] = [-1, c.n_pages]
+    table, kv = _i32(c.table), _i32(kv)
+    n = int(start[-1]) + 3
+    q, k, v = (_rand(rng, (L, n, h, 32), t)[0] for h in (6, 2, 2))
+    f, pos = torch.rand(8, device="cuda"), _i32(rng.integers(0, 1000, n))
+    out = []
+    for bound in (most, None):
+        for given in (None, pos):
+            pools, qo = (c.k.clone(), c.v.clone()), torch.full_like(q, KEEP)
+            mb.cache_append(q, k, v, qo, *pools, table, kv, new_start=_i32(start), max_new=bound, inv_freq=f, positions=given)
+            assert (qo[:, :2] == KEEP).all() and (qo[:, n - 3:] == KEEP).all()
+            out.append((qo, *pools))
+    assert all(torch.equal(a, b) for x, y in ((0, 2), (1, 3)) for a, b in zip(out[x], out[y]))
+    assert not torch.equal(out[0][0], out[1][0]) and not torch.equal(out[0][1], c.k)
+    # starts out of order: rows and places of some sequence or none, nothing else
+    qo = torch.full_like(q, KEEP)
+    mb.cache_append(q, k, v, qo, c.k, c.v, table, kv, new_start=_i32(rng.permutation(start) - 4), inv_freq=f)
+    torch.cuda.synchronize()
+    assert torch.isfinite(qo).all() and torch.isfinite(c.k).all() and torch.isfinite(c.v).all()
+
+
 def test_append_far_positions_and_given_ones():
     """Angles of positions near 2^20 from the places, and of given positions (the
     places then at the sequence's end, as ever)."""
