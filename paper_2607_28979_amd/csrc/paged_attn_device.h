@@ -355,7 +355,7 @@ inline AttendProblem shared_out(AttendProblem p) {
 // single tokens and 512 of one sequence, contexts of 1000, 28 heads on 4 of 128: 96 and 36 us;
 // 200 and 1500 on 1500: 316 and 169; fp32, 47 and 100 on 1000: 81 and 42.
 inline bool scattered(const AttendProblem& p, int rows, int tiles) {
-    return p.c.B <= kMostSeq && (int64_t)p.c.B * p.c.H_kv * tiles > 4 * most_workgroups(shared_out(p), rows);
+    return (int64_t)p.c.B * p.c.H_kv * tiles > 4 * most_workgroups(shared_out(p), rows);
 }
 
 }  // namespace mot
