@@ -494,8 +494,10 @@ typedef struct {
  *     N = { 0 <= v <= u, v > u - window (when window > 0), v in no hole }
  * and zeros where N is empty.  One new token per sequence is a decoding step,
  * many are a chunk of a prompt over what is already cached.  Softmax and
- * accumulation in fp32, o rounded once to dtype (the probabilities of MOT_BF16
- * are rounded to bf16 for the second product, as replay attention does).
+ * accumulation in fp32, o rounded once to dtype.  The second product takes the
+ * probabilities of MOT_BF16 as two bf16 terms (16 bits) where a sequence's rows
+ * are few: max_new H_q / H_kv at most 32, or n_new H_q / H_kv at most 32 B;
+ * elsewhere rounded to bf16, as replay attention does.
  * Positions from kv_len on and holes are not looked at, whatever they hold;
  * a NaN or infinite value reaches the tokens that see it and no others.
  *

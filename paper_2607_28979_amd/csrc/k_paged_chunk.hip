@@ -13,6 +13,12 @@
 // by two-element dot products (436), V of a whole chunk read at once (429).
 // Not kept: the next chunk's scores beside this one's softmax within a wave (it spills at
 // two waves per SIMD, 1061; with one wave 628), in halves (559), priority by workgroup (447).
+//
+// The probabilities are rounded to bf16 for the second product, and a row's sum takes them as
+// rounded, so that the weights add up to 1.  The error against 64 bits is 2.35e-3 of the result,
+// 1.66e-3 of which is the result's own rounding.  As two bf16 terms, a product each, they would
+// leave that alone, at 607 us instead of 413 (1000 tokens on 4000 positions 114 and 91, 6 x 37
+// on 4096 20.9 and 19.5): the products are what bounds this kernel.
 #include "paged_attn_device.h"
 
 namespace mot {

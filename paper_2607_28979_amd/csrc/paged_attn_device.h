@@ -171,6 +171,13 @@ __device__ __forceinline__ float add_bf16x2(uint32_t w, float l) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(two, w), __builtin_bit_cast(two, 0x3f803f80u), l, false);
 }
 
+// Two probabilities as two bf16 terms each (x: rounded, y: the rounded remainders), off by 2^-16
+// of themselves at most.
+__device__ __forceinline__ u32x2 split_bf16x2(float a, float b) {
+    const uint32_t hi = pack_bf16x2(a, b);
+    return {hi, pack_bf16x2(a - bf16_lo(hi), b - bf16_hi(hi))};
+}
+
 // Running softmax of a row: `mo` is the largest exponent so far (base 2), -inf
 // before the first visible position; `base` replaces it where it is -inf.
 __device__ __forceinline__ float base_of(float mo) { return mo == -INFINITY ? 0.f : mo; }

@@ -1,0 +1,46 @@
+"""The paged cache at the edges of what its entry points allow, on the GPU against
+the float64 oracle: how exact the probabilities are, windows and lengths at the
+ends of their ranges, values that are not finite in contexts that are cut, calls
+of very many sequences, rows that end.
+
+Bounds are those of test_gpu_cache.py unless a test says otherwise.
+"""
+import numpy as np
+import pytest
+
+from oracle import cache as ref
+from paper_2607_28979_amd import binding as mb
+
+from test_gpu_cache import HALF, KEEP, Cache, _attend, _bound, _i32, _np, _rand
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("kv,new,Hq,H,D,cut", [
+    ([60, 33, 200], 1, 28, 4, 128, False), ([1500, 90], 1, 12, 2, 128, True), ([150, 77], 4, 14, 2, 64, False),
+    ([100, 300, 40], [3, 10, 0], 14, 2, 64, False), ([100, 300, 40], [3, 11, 0], 14, 2, 64, False), ([2000] + [50] * 7, [40] + [1] * 7, 8, 2, 64, True)])
+def test_probabilities_of_few_rows(kv, new, Hq, H, D, cut):
+    """Tiles of 32 rows: a probability is off by 2^-16 of itself at most (two bf16 terms, the second's
+    rounding 2^-8 of at most 2^-8), so the result by 2^-16 of sum of softmax |v| beside its own rounding and
+    the fp32 steps.  14 tokens of 7 query heads are 98 rows, more than the 32 of each of 3 sequences: those
+    probabilities are rounded once, and the bound is that of tiles of 128 rows."""
+    import torch
+    rng = np.random.default_rng(sum(kv))
+    c = Cache(rng, kv, 16, H, D, "bf16", max_pages=256 if cut else None)
+    packed = isinstance(new, list)
+    q, _ = _rand(rng, ((sum(new),) if packed else (len(kv), new)) + (Hq, D), "bf16")
+    start = np.concatenate([[0], np.cumsum(new)]) if packed else None
+    o = torch.full_like(q, KEEP)
+    print("case probabilities", kv, new, cut, flush=True)
+    mb.paged_attention(q, c.k, c.v, c.d_table, c.d_kv, o, new_start=None if start is None else _i32(start))
+    flat = (int(np.prod(q.shape[:-2])), Hq, D)
+    want, mag, smax = ref.paged_attention(_np(q).reshape(flat), *c.host(), c.table, c.kv, np.full(flat, KEEP), start,
+                                          flat[0] if packed else new)
+    most = flat[0] if packed else new
+    few = most * (Hq // H) <= 32 or flat[0] * (Hq // H) <= 32 * len(kv)
+    assert few == (new != [3, 11, 0])
+    bound = HALF["bf16"] * np.abs(want) + mag * (2.0 ** -16 + (2 * (D + 4) * smax + 2 * (max(kv) + 8)) * 2.0 ** -24) + 1e-30
+    if not few:
+        bound = _bound("bf16", want, mag, smax, D, max(kv), True)
+    bad = ~(np.abs(_np(o).reshape(flat) - want) <= bound)
+    assert not bad.any(), (int(bad.sum()), bad.size)
