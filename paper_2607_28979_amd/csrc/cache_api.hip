@@ -144,8 +144,10 @@ AttendProblem attend_problem(const mot_cache_shapes* c, const mot_attend_shapes*
     p.c.n_new = s->n_new;
     p.c.max_new = s->max_new;
     p.H_q = s->H_q;
-    p.window = s->window;
     const int most = c->max_pages * c->page_size;
+    // A window of every position there can be is none.  Shorter ones are under 2^30, and new tokens
+    // lie at -2^26 or later, so u - window fits in 32 bits.
+    p.window = s->window < most ? s->window : 0;
     p.max_kv = s->max_kv > 0 && s->max_kv < most ? s->max_kv : most;
     p.scale_log2 = (float)((s->scale > 0.f ? (double)s->scale : 1.0 / sqrt((double)c->D)) * 1.4426950408889634);
     p.qs = strides(s->q);

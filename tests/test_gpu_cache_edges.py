@@ -44,3 +44,21 @@ def test_probabilities_of_few_rows(kv, new, Hq, H, D, cut):
         bound = _bound("bf16", want, mag, smax, D, max(kv), True)
     bad = ~(np.abs(_np(o).reshape(flat) - want) <= bound)
     assert not bad.any(), (int(bad.sum()), bad.size)
+
+
+@pytest.mark.parametrize("t,n,Hq,D", [("bf16", 3, 6, 64), ("bf16", 30, 4, 64), ("bf16", 30, 28, 128), ("f32", 30, 4, 64), ("f32", 7, 2, 128)])
+def test_windows_longer_than_the_context(t, n, Hq, D):
+    """A window as long as an int goes is no window, also where new tokens lie at negative
+    positions (more of them than positions); so is one of all positions of a table's row, one more,
+    one less."""
+    import torch
+    rng = np.random.default_rng(n)
+    kv = [20, 1, 28, 0, 2]
+    print("case windows", t, n, flush=True)
+    for wide in (None, 256):
+        c = Cache(rng, kv, 16, 2, D, t, max_pages=wide)
+        most = c.table.shape[1] * 16
+        q, _ = _rand(rng, (5, n, Hq, D), t)
+        none = _attend(c, q)
+        for w in (2 ** 31 - 1, 2 ** 31 - 2, 2 ** 30, most + 1, most, most - 1):
+            assert torch.equal(_attend(c, q, window=w), none), (w, most)
