@@ -611,7 +611,9 @@ mot_status mot_cache_append(const void* q, const void* k, const void* v, void* q
  * free: a page is in use when the table names it, nothing else is kept.
  *
  *   table        device int32 [B][max_pages], read
- *   source       device int32 [n_rows]; outside 0 .. B - 1: an empty row
+ *   source       device int32 [n_rows]; outside 0 .. B - 1: an empty row, which
+ *                keeps nothing (keep is not looked at) but still gets room for
+ *                want: a new prompt's pages
  *   keep, want   device int32 [n_rows], cut to 0 .. max_pages * page_size;
  *                want below keep means keep.  keep is at most what the source
  *                row holds; holes among the kept pages stay holes
@@ -622,8 +624,9 @@ mot_status mot_cache_append(const void* q, const void* k, const void* v, void* q
  *   workspace    device scratch of this call, at least mot_cache_workspace_bytes
  *                (16-byte aligned, not overlapping its arrays; calls that
  *                overlap in time need their own); not looked at where that is 0
- * Beam search sets source to the parents and want = keep + 1; a beam that ends
- * has source -1.  n_rows at most 4096 (0: a no-op that writes nothing).  The
+ * Beam search sets source to the parents and want = keep + 1; a row that ends
+ * (a finished beam or sequence) has source -1 and want 0, else it would take
+ * want's pages anew.  n_rows at most 4096 (0: a no-op that writes nothing).  The
  * data of pages that new rows take over does not move.
  */
 mot_status mot_cache_reorder(void* k_pages, void* v_pages, const int32_t* table, const int32_t* source,

@@ -712,7 +712,8 @@ def cache_reorder(k_pages, v_pages, table, source, keep, want, new_table, missin
                   workspace=None) -> None:
     """mot_cache_reorder on the current torch stream: row b of new_table takes the
     first keep[b] positions of row source[b] of table and room for want[b]
-    (int32 [n_rows] each; missing: int32 [1], output).  workspace None: torch
+    (int32 [n_rows] each; missing: int32 [1], output).  source -1: nothing is
+    kept; a row that ends has want 0 too, a new prompt's its length.  workspace None: torch
     memory of this call."""
     lib, _ = _ready()
     c = _Pools(k_pages, v_pages, table, page_layout)

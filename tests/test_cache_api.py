@@ -259,3 +259,14 @@ def test_oracle_compact_by_hand():
     k, v, new, n = ref.cache_compact(pool, pool, np.array([[5, 1], [5, -1], [4, 9]]))
     assert n == 3 and new.tolist() == [[2, 1], [2, -1], [0, -1]]
     assert k.ravel().tolist() == [4, 1, 5, 3, 4, 5]
+
+
+def test_oracle_reorder_of_rows_that_end():
+    """A row that ends (source -1, want 0) holds no page and misses none; with want left at
+    its length it takes pages anew."""
+    pool = np.zeros((1, 4, 16, 1, 1))
+    table = np.array([[0, 1, -1], [2, 3, -1]])
+    new, missing = ref.cache_reorder(pool, pool, table, [0, -1], [20, 20], [21, 0])[2:]
+    assert new.tolist() == [[0, 1, -1], [-1, -1, -1]] and missing == 0
+    new, missing = ref.cache_reorder(pool, pool, table, [0, -1], [20, 20], [21, 40])[2:]
+    assert new.tolist() == [[0, 1, -1], [2, 3, -1]] and missing == 1

@@ -62,3 +62,30 @@ def test_windows_longer_than_the_context(t, n, Hq, D):
         none = _attend(c, q)
         for w in (2 ** 31 - 1, 2 ** 31 - 2, 2 ** 30, most + 1, most, most - 1):
             assert torch.equal(_attend(c, q, window=w), none), (w, most)
+
+
+@pytest.mark.parametrize("spare", [40, 17000])
+def test_rows_that_end_hold_no_page(spare):
+    """Beams go on from their parents for many steps in a pool that has no page to lose, and half of
+    them end on the way: source -1 and want 0 leaves a row without pages, whatever keep says, and none
+    is ever missing."""
+    import torch
+    rng = np.random.default_rng(spare)
+    B, ps = 8, 16
+    c = Cache(rng, [50] * B, ps, 1, 16, "bf16", L=1, spare=spare, stale=False, max_pages=6)
+    table, live, at = c.table, np.ones(B, bool), 50
+    for step in range(40):
+        if step in (3, 9, 20, 21):
+            live[rng.choice(np.flatnonzero(live))] = False
+        parents = np.flatnonzero(live)
+        src = np.where(live, rng.choice(parents, B), -1)
+        keep, want = np.full(B, at), np.where(live, at + 1, 0)
+        new, missing = torch.full((B, 6), 77, dtype=torch.int32, device="cuda"), _i32([-1])
+        k, v = c.host()
+        mb.cache_reorder(c.k, c.v, _i32(table), _i32(src), _i32(keep), _i32(want), new, missing)
+        wk, wv, wt, wm = ref.cache_reorder(k, v, table, src, keep, want)
+        new = new.cpu().numpy()
+        assert np.array_equal(new, wt) and int(missing) == wm == 0
+        assert np.array_equal(_np(c.k), wk) and np.array_equal(_np(c.v), wv)
+        assert (new[~live] == -1).all() and (new[live, :-(-(at + 1) // ps)] >= 0).all()
+        table, live, at = new, src >= 0, at + 1
