@@ -56,6 +56,7 @@ struct AttendProblem {
     int32_t H_q, window;
     int32_t n_split, least;  // workgroups that share the work (1: they do not), blocks of a share at least
     int32_t max_kv;          // bound on kv_len that the cuts go by
+    int32_t wide;            // sums over the sequences may pass 32 bits
     float scale_log2;        // scale * log2(e)
     RowStrides qs, os;
 };
@@ -84,7 +85,7 @@ struct PagesProblem {
     void* ws;
 };
 
-// Sets p.n_split and p.least; the bytes of `part` that they need (0: nothing is cut).
+// Sets p.n_split, p.least and p.wide; the bytes of `part` that they need (0: nothing is cut).
 size_t attend_plan(AttendProblem& p, bool bf16);
 hipError_t launch_paged_attention(const AttendProblem& p, bool bf16, hipStream_t stream);
 // bf16 calls whose sequences have a tile of 32 query rows at most per KV head

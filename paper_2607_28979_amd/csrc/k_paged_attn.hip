@@ -129,13 +129,13 @@ size_t attend_plan(AttendProblem& p, bool bf16) {
     const int rows = tile_rows(p, bf16), step = rows == 128 ? 64 : 32, B = min(p.c.B, kMostSeq);
     p.n_split = 1;
     p.least = 4;   // blocks: one per wave, or four chunks
+    // all tiles' blocks, whatever the lengths and starts hold
+    const int64_t blocks = (((int64_t)p.c.max_pages << p.c.page_shift) + step - 1) / step + 1;
+    const int64_t tiles = ((int64_t)p.c.max_new * (p.H_q / p.c.H_kv) + rows - 1) / rows;
+    p.wide = (double)B * p.c.H_kv * tiles * blocks > 1 << 30;
     const int64_t whole = most_workgroups(p, rows) - 1;   // workgroups of the call uncut
     if (rows == 32 ? p.max_kv <= 1024 : rows == 128 ? whole >= 192 || p.max_kv <= 512 + 8 * whole
                                                     : whole >= 512 || p.max_kv <= 512) return 0;
-    // sums of all tiles' blocks stay in 32 bits, whatever the lengths and starts hold
-    const int64_t blocks = (((int64_t)p.c.max_pages << p.c.page_shift) + step - 1) / step + 1;
-    const int64_t tiles = ((int64_t)p.c.max_new * (p.H_q / p.c.H_kv) + rows - 1) / rows;
-    if ((double)B * p.c.H_kv * tiles * blocks > INT32_MAX) return 0;
     p.n_split = !bf16 || p.c.D == 128 ? 448 : 704;
     const size_t R = (size_t)partial_of(p, rows).R;
     return 2 * p.n_split * R * (p.c.D + 2) * sizeof(float) + (size_t)B * p.c.H_kv * sizeof(int2);

@@ -232,6 +232,40 @@ __device__ __forceinline__ void span_of(const AttendProblem& p, Work& w, int ste
 // that any run of them is about the same work.
 __device__ __forceinline__ int mixed_tile(int i, int n) { return i & 1 ? i >> 1 : n - 1 - (i >> 1); }
 
+// The share of a call, and the workgroups (`cuts`: those of cut sequences) of this lane's
+// sequences.  I: 32 bits, or 64 where sums of a call's sizes may pass that (p.wide; 64 bits
+// throughout cost a decoding step 0.3 us).  False: more workgroups than a launch holds, which
+// only starts that do not ascend ask for (their rows are unspecified).
+template <typename I, int N>
+__device__ __forceinline__ bool shares_of(const AttendProblem& p, const int (&blocks)[N], const int (&tiles)[N], int& share, int& mine,
+                                          int& cuts) {
+    share = p.least;
+    if (p.part) {
+        I sum = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += (I)blocks[i] * tiles[i];
+        if constexpr (sizeof(I) == 4) {
+            share = max(div_up(__builtin_amdgcn_readlane(wave_scan(sum), 63) * p.c.H_kv, p.n_split), share);
+        } else {
+            // multiples of 2^20 and the rest; from 2^44 blocks on the share is longer than any sequence
+            const int high = (int)min(sum >> 20, (I)1 << 24), low = (int)(sum & ((1 << 20) - 1));
+            const I total = ((I)__builtin_amdgcn_readlane(wave_scan(high), 63) << 20) + __builtin_amdgcn_readlane(wave_scan(low), 63);
+            share = max((int)min((total * p.c.H_kv + p.n_split - 1) / p.n_split, (I)1 << 30), share);
+        }
+    }
+    I all = 0, cut = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int parts = div_up(blocks[i], share);
+        const I n = (I)parts * tiles[i] * p.c.H_kv;
+        all += n;
+        cut += parts > 1 ? n : 0;
+    }
+    mine = (int)all;
+    cuts = (int)cut;
+    return sizeof(I) == 4 || !__builtin_amdgcn_ballot_w64(all > 1 << 24);
+}
+
 // N sequences per lane (lane i: N i .. N i + N - 1).  False: none for this workgroup.  Where
 // sequences have several tiles the workgroups of an XCD (every eighth) take neighbouring
 // ones, so that the tiles of one (sequence, KV head, part) meet its K and V in one L2.
@@ -239,7 +273,7 @@ template <int N>
 __device__ __forceinline__ bool shared_work(const AttendProblem& p, int rows, int step, bool by_xcd, Work& w) {
     const int lane = threadIdx.x & 63, H = p.c.H_kv, G = p.H_q / H;
     NewTokens nt[N];
-    int blocks[N], tiles[N], sum = 0;
+    int blocks[N], tiles[N], share, mine, cuts;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int s = lane * N + i;
@@ -247,17 +281,9 @@ __device__ __forceinline__ bool shared_work(const AttendProblem& p, int rows, in
         nt[i] = new_tokens(p.c, min(s, p.c.B - 1));
         blocks[i] = s < p.c.B ? blocks_of(p, nt[i], step, &from) : 0;
         tiles[i] = div_up(nt[i].n * G, rows);
-        sum += blocks[i] * tiles[i];
     }
-    const int total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
-    const int share = p.part ? max(div_up(total * H, p.n_split), p.least) : p.least;
-    int mine = 0, cuts = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int parts = div_up(blocks[i], share), n = parts * tiles[i] * H;
-        mine += n;
-        cuts += parts > 1 ? n : 0;
-    }
+    if (!(__builtin_expect(p.wide, 0) ? shares_of<int64_t>(p, blocks, tiles, share, mine, cuts) : shares_of<int>(p, blocks, tiles, share, mine, cuts)))
+        return false;
     const int upto = wave_scan(mine), cutto = wave_scan(cuts);
     int id = blockIdx.x;
     if (by_xcd) {

@@ -270,3 +270,18 @@ def test_oracle_reorder_of_rows_that_end():
     assert new.tolist() == [[0, 1, -1], [-1, -1, -1]] and missing == 0
     new, missing = ref.cache_reorder(pool, pool, table, [0, -1], [20, 20], [21, 40])[2:]
     assert new.tolist() == [[0, 1, -1], [2, 3, -1]] and missing == 1
+
+
+@pytest.mark.parametrize("B,n_new,max_new,H_q,H_kv,D,max_pages,ps,dtype,cut", [
+    (512, 4096, 4096, 32, 8, 64, 2048, 16, mb.MOT_BF16, True),      # many sequences, a loose bound on their tokens
+    (600, 1000, 1000, 28, 4, 128, 8192, 64, mb.MOT_BF16, True), (70, 70, 1, 2, 2, 64, 1 << 14, 1024, mb.MOT_BF16, True),
+    (64, 64, 64, 16, 16, 64, 1 << 14, 1024, mb.MOT_F32, False), (2, 37, 37, 28, 4, 128, 1 << 20, 1024, mb.MOT_BF16, True),
+    (20, 64, 64, 16, 16, 64, 1 << 16, 1024, mb.MOT_F32, True)])
+def test_long_contexts_are_cut_whatever_the_table_holds(lib, B, n_new, max_new, H_q, H_kv, D, max_pages, ps, dtype, cut):
+    """Tables of wide rows, many sequences and loose bounds do not keep a long sequence whole; what does
+    (fp32) is as many tiles as fill the chip: up to 64 / 16 + 64 of them on 16 heads are 1088, from 512 on
+    nothing is cut."""
+    c = _cache(B=B, H_kv=H_kv, D=D, max_pages=max_pages, page_size=ps, dtype=dtype)
+    s = mb._AttendShapes(n_new, max_new, H_q, 0, 0, 0.0, _rows(H_q, D, n_new), _rows(H_q, D, n_new))
+    need = lib.mot_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(s))
+    assert (0 < need < 1 << 30) if cut else need == 0

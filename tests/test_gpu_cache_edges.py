@@ -89,3 +89,60 @@ def test_rows_that_end_hold_no_page(spare):
         assert np.array_equal(_np(c.k), wk) and np.array_equal(_np(c.v), wv)
         assert (new[~live] == -1).all() and (new[live, :-(-(at + 1) // ps)] >= 0).all()
         table, live, at = new, src >= 0, at + 1
+
+
+@pytest.mark.parametrize("B,n,Hq,H,D,t", [(1, 1, 6, 2, 64, "bf16"), (70, 1, 4, 1, 128, "bf16"), (1, 37, 6, 2, 64, "bf16"),
+                                          (70, 37, 4, 1, 128, "bf16"), (1, 1, 6, 2, 64, "f32"), (66, 1, 4, 2, 64, "f32")])
+def test_positions_to_the_end_of_the_range(B, n, Hq, H, D, t):
+    """One sequence of nearly 2^30 positions, nearly all of them holes, alone and among short ones: its
+    blocks are more than 32 bits hold for all sequences and heads, and it is still cut."""
+    import torch
+    ps, M, kv0 = 1024, 1 << 20, (1 << 30) - 7
+    print("case far", B, n, t, flush=True)
+    rng = np.random.default_rng(B + n)
+    held = np.array([0, 3, 65537, 999999, M - 1])                # entries of the long row that are pages
+    k, v = (_rand(rng, (len(held) + B, ps, H, D), t)[0] for _ in range(2))
+    pages = rng.permutation(len(held) + B)
+    table = torch.full((B, M), -1, dtype=torch.int32, device="cuda")
+    long = B // 2
+    table[long, torch.from_numpy(held).cuda()] = _i32(pages[:len(held)])
+    lens = rng.integers(1, 200, B)
+    lens[long] = kv0
+    for b in range(B):
+        if b != long:
+            table[b, 0] = int(pages[len(held) + b])
+    q, _ = _rand(rng, (B, n, Hq, D), t)
+    o = torch.full_like(q, KEEP)
+    mb.paged_attention(q, k, v, table, _i32(lens), o)
+    torch.cuda.synchronize()
+    pos = torch.from_numpy((held[:, None] * ps + np.arange(ps)[None]).reshape(-1)).cuda()
+    for b in sorted({0, long, B - 1}):
+        at = pos if b == long else torch.arange(ps, device="cuda")
+        ids = torch.from_numpy(pages[:len(held)]).cuda() if b == long else pages[len(held) + b:len(held) + b + 1]
+        K, V = (x[ids].reshape(-1, H, D).double() for x in (k, v))
+        for h in range(Hq):
+            u = int(lens[b]) - n + torch.arange(n, device="cuda")
+            s = (q[b, :, h].double() @ K[:, h * H // Hq].T) / D ** 0.5
+            s.masked_fill_(at[None] > u[:, None], -float("inf"))
+            p = torch.nan_to_num(torch.softmax(s, -1))            # a token at a negative position sees none
+            want, mag = p @ V[:, h * H // Hq], p @ V[:, h * H // Hq].abs()
+            smax = (q[b, :, h].double().abs() @ K[:, h * H // Hq].abs().T).amax() / D ** 0.5
+            bound = _bound(t, _np(want), _np(mag), float(smax), D, len(held) * ps, t == "bf16" and n * Hq // H > 32)
+            assert (np.abs(_np(o[b, :, h]) - _np(want)) <= bound).all(), (b, h)
+
+
+def test_many_sequences_a_loose_bound_and_a_wide_table():
+    """512 sequences, 4096 rows of tokens, no bound on a sequence's: the one of 9000 positions is cut."""
+    import torch
+    rng = np.random.default_rng(9)
+    B = 512
+    counts = rng.integers(0, 2, B)
+    counts[[0, 300, B - 1]] = 1, 3, 5
+    kv = counts + rng.integers(0, 20, B)
+    kv[300] = 9000
+    c = Cache(rng, kv.tolist(), 16, 8, 64, "bf16", stale=False, max_pages=2048)
+    q, _ = _rand(rng, (4096, 32, 64), "bf16")
+    print("case wide", flush=True)
+    whole = _attend(c, q, counts.tolist(), scratch=False)
+    cut = _attend(c, q, counts.tolist())
+    assert (cut[int(counts.sum()):] == KEEP).all() and not torch.equal(whole, cut)
