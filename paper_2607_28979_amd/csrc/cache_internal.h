@@ -88,11 +88,11 @@ struct PagesProblem {
 // Sets p.n_split, p.least and p.wide; the bytes of `part` that they need (0: nothing is cut).
 size_t attend_plan(AttendProblem& p, bool bf16);
 hipError_t launch_paged_attention(const AttendProblem& p, bool bf16, hipStream_t stream);
-// bf16 calls whose sequences have a tile of 32 query rows at most per KV head
-// (k_paged_decode.hip), more (k_paged_chunk.hip), and fp32 ones (k_paged_f32.hip)
-hipError_t launch_paged_decode(const AttendProblem& p, hipStream_t stream);
-hipError_t launch_paged_chunk(const AttendProblem& p, hipStream_t stream);
-hipError_t launch_paged_f32(const AttendProblem& p, hipStream_t stream);
+// bf16 calls on tiles of 32 query rows (k_paged_decode.hip), of 128 (k_paged_chunk.hip), and fp32
+// ones, of 16 (k_paged_f32.hip).  finds: the workgroups find their work, of 512 sequences at most
+hipError_t launch_paged_decode(const AttendProblem& p, bool finds, hipStream_t stream);
+hipError_t launch_paged_chunk(const AttendProblem& p, bool finds, hipStream_t stream);
+hipError_t launch_paged_f32(const AttendProblem& p, bool finds, hipStream_t stream);
 hipError_t launch_cache_append(const AppendProblem& p, bool bf16, hipStream_t stream);
 // n_rows: of a reordering, 0: compaction; rows x max_pages: entries of the new table (0 bytes:
 // the plan fits a workgroup's LDS)

@@ -7,32 +7,14 @@ namespace mot {
 namespace {
 
 // The partial sums of a cut (sequence, KV head), brought to one base and added, in the order
-// of the parts within each of the groups of D / 4 threads, then of the groups.  A
-// workgroup per query row, four parts' loads of every group under way together: it is all
-// latency (48 tokens of 28 heads over up to 8192 positions: 4.8 us; one token: 3.4).
-// grid (max_new * H_q, B), or by_row (n_new * H_q) of packed tokens, whose sequence every
-// wave finds among the starts; rows: of a tile
+// of the parts within each of the groups of D / 4 threads, then of the groups: query head h
+// of new token t of sequence b, by a workgroup.  Four parts' loads of every group are under
+// way together: it is all latency (48 tokens of 28 heads over up to 8192 positions: 4.8 us;
+// one token: 3.4).  rows: of a tile
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_paged_join(AttendProblem p, int rows, bool by_row) {
+__device__ __forceinline__ void join_row(const AttendProblem& p, int rows, int b, int t, int h, f32x4* s_acc, float2* s_ml) {
     constexpr int TH = D / 4, NG = 256 / TH;   // threads of a group, groups
-    __shared__ f32x4 s_acc[256];
-    __shared__ float2 s_ml[NG];
-    const int G = p.H_q / p.c.H_kv, h = blockIdx.x % p.H_q, kvh = h / G;
-    int b = blockIdx.y, t = blockIdx.x / p.H_q;
-    if (by_row) {
-        const int lane = threadIdx.x & 63, row = t;
-        b = -1;
-        for (int b0 = 0; b0 < p.c.B && b < 0; b0 += 64) {
-            const NewTokens nt = new_tokens(p.c, min(b0 + lane, p.c.B - 1));
-            const unsigned long long here = __builtin_amdgcn_ballot_w64(b0 + lane < p.c.B && row >= nt.row && row < nt.row + nt.n);
-            if (here) {
-                const int who = __builtin_ctzll(here);
-                b = b0 + who;
-                t = row - __builtin_amdgcn_readlane(nt.row, who);
-            }
-        }
-        if (b < 0) return;   // uniform over the workgroup
-    }
+    const int G = p.H_q / p.c.H_kv, kvh = h / G;
     const int c = threadIdx.x % TH, grp = threadIdx.x / TH;
     const Partial pt = partial_of(p, rows);
     const int2 span = pt.span[b * p.c.H_kv + kvh];
@@ -101,6 +83,31 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendProblem p, int rows, b
         *reinterpret_cast<f32x4*>(o) = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
 }
 
+// grid (max_new * H_q, B), or by_row (some rows * H_q) of packed tokens: the rows between the
+// slice's first start and its last, whose sequences every wave finds among the starts.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_paged_join(AttendProblem p, int rows, bool by_row) {
+    __shared__ f32x4 s_acc[256];
+    __shared__ float2 s_ml[1024 / D];
+    const int h = blockIdx.x % p.H_q, t = blockIdx.x / p.H_q;
+    if (!by_row) {
+        join_row<T, D>(p, rows, blockIdx.y, t, h, s_acc, s_ml);
+        return;
+    }
+    const int lane = threadIdx.x & 63, end = min(p.c.start[p.c.B], p.c.n_new), step = gridDim.x / p.H_q;
+    for (int row = max(p.c.start[0], 0) + t; row < end; row += step) {
+        for (int b0 = 0; b0 < p.c.B; b0 += 64) {
+            const NewTokens nt = new_tokens(p.c, min(b0 + lane, p.c.B - 1));
+            const unsigned long long here = __builtin_amdgcn_ballot_w64(b0 + lane < p.c.B && row >= nt.row && row < nt.row + nt.n);
+            if (!here) continue;   // uniform over the workgroup
+            const int who = __builtin_ctzll(here);
+            join_row<T, D>(p, rows, b0 + who, row - __builtin_amdgcn_readlane(nt.row, who), h, s_acc, s_ml);
+            break;
+        }
+        __syncthreads();   // the sums are read: the next row's may be written
+    }
+}
+
 // Rows of a tile: 32 where all of a sequence's fit, or an average one's do (packed tokens
 // with a loose max_new), else 128; fp32 16.  With no max_new, 128 and 32 rows: 48 single
 // tokens on 4000 114 and 86 us, 256 on 300 66 and 42, 32 x 4 on 2000 118 and 41, 47 and 100 of
@@ -143,11 +150,17 @@ size_t attend_plan(AttendProblem& p, bool bf16) {
 
 namespace {
 
-hipError_t launch_slice(const AttendProblem& p, bool bf16, int rows, hipStream_t stream) {
-    hipError_t e = rows == 32 ? launch_paged_decode(p, stream) : bf16 ? launch_paged_chunk(p, stream) : launch_paged_f32(p, stream);
+// slices: of the call
+hipError_t launch_slice(const AttendProblem& p, bool bf16, int rows, bool finds, int slices, hipStream_t stream) {
+    hipError_t e = rows == 32 ? launch_paged_decode(p, finds, stream)
+                   : bf16     ? launch_paged_chunk(p, finds, stream)
+                              : launch_paged_f32(p, finds, stream);
     if (e != hipSuccess || !p.part) return e;
     const bool by_row = p.c.start && (int64_t)p.c.max_new * p.c.B > 2 * (int64_t)p.c.n_new;
-    const dim3 join((by_row ? p.c.n_new : p.c.max_new) * p.H_q, by_row ? 1 : p.c.B);
+    // packed rows: a slice's share of the call's, and its workgroups walk further where it has more
+    // (4096 single tokens without a bound, one on 9000 positions: 803 us; every slice with a
+    // workgroup for every row of the call 1680)
+    const dim3 join((by_row ? div_up(p.c.n_new, slices) : p.c.max_new) * p.H_q, by_row ? 1 : p.c.B);
     if (bf16 && p.c.D == 128) k_paged_join<uint16_t, 128><<<join, 256, 0, stream>>>(p, rows, by_row);
     else if (bf16) k_paged_join<uint16_t, 64><<<join, 256, 0, stream>>>(p, rows, by_row);
     else if (p.c.D == 128) k_paged_join<float, 128><<<join, 256, 0, stream>>>(p, rows, by_row);
@@ -157,13 +170,17 @@ hipError_t launch_slice(const AttendProblem& p, bool bf16, int rows, hipStream_t
 
 }  // namespace
 
-// As many sequences at a time as a workgroup adds up; the slices share the workspace, one
-// after the other.  599 single tokens on 300 positions and one on 30000: 365 us whole, 138 so.
+// Workgroups that find their work add up as many sequences at a time as fit in a wave's
+// lanes; the slices share the workspace, one after the other.  599 single tokens on 300
+// positions and one on 30000: 365 us whole, 138 so.  Where each has a tile of its own, all
+// sequences are one launch: 4096 single tokens on 100 positions 224 us, in slices 251.
 hipError_t launch_paged_attention(const AttendProblem& p, bool bf16, hipStream_t stream) {
     const int rows = tile_rows(p, bf16);
-    for (int b0 = 0; b0 < p.c.B; b0 += kMostSeq) {
+    const bool finds = finds_work(p, rows);
+    const int most = finds ? kMostSeq : p.c.B;
+    for (int b0 = 0; b0 < p.c.B; b0 += most) {
         AttendProblem s = p;
-        s.c.B = min(p.c.B - b0, kMostSeq);
+        s.c.B = min(p.c.B - b0, most);
         s.c.table += (int64_t)b0 * p.c.max_pages;
         s.c.kv_len += b0;
         if (p.c.start) {
@@ -174,7 +191,7 @@ hipError_t launch_paged_attention(const AttendProblem& p, bool bf16, hipStream_t
             s.o = reinterpret_cast<char*>(p.o) + bytes * p.os.batch;
             s.c.n_new = s.c.B * p.c.max_new;
         }
-        const hipError_t e = launch_slice(s, bf16, rows, stream);
+        const hipError_t e = launch_slice(s, bf16, rows, finds, div_up(p.c.B, most), stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

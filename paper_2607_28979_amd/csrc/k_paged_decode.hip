@@ -267,9 +267,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
 }
 
 template <int D>
-hipError_t launch_d(const AttendProblem& p, hipStream_t stream) {
+hipError_t launch_d(const AttendProblem& p, bool finds, hipStream_t stream) {
     const int whole = p.c.B * p.c.H_kv;
-    if (p.part || (int64_t)p.c.max_new * (p.H_q / p.c.H_kv) > 32) {
+    if (finds) {
         const AttendProblem s = shared_out(p);
         const int64_t grid = most_workgroups(s, 32);
         if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
@@ -286,8 +286,8 @@ hipError_t launch_d(const AttendProblem& p, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_paged_decode(const AttendProblem& p, hipStream_t stream) {
-    return p.c.D == 128 ? launch_d<128>(p, stream) : launch_d<64>(p, stream);
+hipError_t launch_paged_decode(const AttendProblem& p, bool finds, hipStream_t stream) {
+    return p.c.D == 128 ? launch_d<128>(p, finds, stream) : launch_d<64>(p, finds, stream);
 }
 
 }  // namespace mot

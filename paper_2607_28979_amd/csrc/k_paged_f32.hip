@@ -244,13 +244,12 @@ __global__ __launch_bounds__(256, 2) void k_paged_f32(AttendProblem p, int tiles
 }
 
 template <int D>
-hipError_t launch_d(const AttendProblem& p, hipStream_t stream) {
+hipError_t launch_d(const AttendProblem& p, bool finds, hipStream_t stream) {
     const int tiles = div_up(p.c.max_new * (p.H_q / p.c.H_kv), 16);
-    const bool own = !p.part && !scattered(p, 16, tiles);
     const AttendProblem s = shared_out(p);
-    const int64_t grid = ((own ? (int64_t)p.c.B * p.c.H_kv * tiles : most_workgroups(s, 16)) + 7) / 8 * 8;
+    const int64_t grid = ((finds ? most_workgroups(s, 16) : (int64_t)p.c.B * p.c.H_kv * tiles) + 7) / 8 * 8;
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-    if (own) k_paged_f32<D, 0><<<(unsigned)grid, 256, 0, stream>>>(p, tiles);
+    if (!finds) k_paged_f32<D, 0><<<(unsigned)grid, 256, 0, stream>>>(p, tiles);
     else if (p.c.B <= 64) k_paged_f32<D, 1><<<(unsigned)grid, 256, 0, stream>>>(s, tiles);
     else k_paged_f32<D, kSeqPerLane><<<(unsigned)grid, 256, 0, stream>>>(s, tiles);
     return hipGetLastError();
@@ -258,8 +257,8 @@ hipError_t launch_d(const AttendProblem& p, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_paged_f32(const AttendProblem& p, hipStream_t stream) {
-    return p.c.D == 128 ? launch_d<128>(p, stream) : launch_d<64>(p, stream);
+hipError_t launch_paged_f32(const AttendProblem& p, bool finds, hipStream_t stream) {
+    return p.c.D == 128 ? launch_d<128>(p, finds, stream) : launch_d<64>(p, finds, stream);
 }
 
 }  // namespace mot

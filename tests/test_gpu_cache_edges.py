@@ -5,6 +5,8 @@ of very many sequences, rows that end.
 
 Bounds are those of test_gpu_cache.py unless a test says otherwise.
 """
+from types import SimpleNamespace
+
 import numpy as np
 import pytest
 
@@ -146,3 +148,41 @@ def test_many_sequences_a_loose_bound_and_a_wide_table():
     whole = _attend(c, q, counts.tolist(), scratch=False)
     cut = _attend(c, q, counts.tolist())
     assert (cut[int(counts.sum()):] == KEEP).all() and not torch.equal(whole, cut)
+
+
+def _kernels(call):
+    """Nodes of the graph that `call` is captured into."""
+    import ctypes
+    import torch
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(g):
+        call()
+    n = ctypes.c_size_t(0)
+    hip = ctypes.CDLL(next(iter(mb._hip_runtimes())))
+    assert hip.hipGraphGetNodes(ctypes.c_void_p(g.raw_cuda_graph()), None, ctypes.byref(n)) == 0
+    return n.value
+
+
+@pytest.mark.parametrize("t,B,n,D", [("bf16", 2000, 1, 128), ("bf16", 1500, 9, 64), ("f32", 1300, 4, 64), ("bf16", 65535, 1, 64)])
+def test_many_short_sequences_are_one_launch(t, B, n, D):
+    """Calls that cut nothing take any number of sequences at once, with the bits of calls of some each."""
+    import torch
+    rng = np.random.default_rng(B)
+    print("case short", t, B, n, flush=True)
+    c = Cache(rng, [5, 3, 40, 0], 16, 2, D, t, stale=False)
+    pick = rng.integers(0, 4, B)
+    table, kv = _i32(c.table[pick]), _i32(np.array(c.kv)[pick])
+    q, _ = _rand(rng, (B, n, 8, D), t)
+    o = torch.full_like(q, KEEP)
+    assert _kernels(lambda: mb.paged_attention(q, c.k, c.v, table, kv, o)) == 1
+    parts = torch.full_like(q, KEEP)
+    for at in range(0, B, 500):
+        m = slice(at, min(at + 500, B))
+        mb.paged_attention(q[m], c.k, c.v, table[m], kv[m], parts[m])
+    assert torch.equal(o, parts) and (o[:, :] != KEEP).all()
+    some = [int(np.flatnonzero(pick == i)[-1]) for i in range(4)]
+    few = SimpleNamespace(k=c.k, v=c.v, layout=0, host=c.host, table=c.table[pick[some]], kv=[c.kv[i] for i in pick[some]],
+                          d_table=table[some].contiguous(), d_kv=kv[some].contiguous())
+    assert torch.equal(_attend(few, q[some].contiguous()), o[some])
