@@ -459,7 +459,8 @@ mot_status mot_backbone_translate(const void* src_k, const void* src_v, const in
  *
  * New token i of the c of sequence b is at position kv_len[b] - c + i.  Rows
  * of no sequence are left as they are, and so are, of a sequence with more
- * than max_new new tokens, those from the max_new-th on.
+ * than max_new new tokens, those from the max_new-th on.  A call takes at most
+ * 2^26 - 32 new tokens.
  *
  *   L            layers of the pools (1..MOT_MAX_LAYERS)
  *   n_pages      pages of a layer's pool
@@ -522,7 +523,9 @@ typedef struct {
  *                workgroups, whose partial sums a second kernel joins in a
  *                fixed order; with less, or NULL, no sequence is cut (same
  *                results up to the order of fp32 sums)
- * D is 64 or 128 (else MOT_ERR_UNSUPPORTED).  n_new = 0 and B = 0 are no-ops.
+ * D is 64 or 128 (else MOT_ERR_UNSUPPORTED, as are more tiles of query rows
+ * than a launch holds: from 2^28 rows of a sequence in fp32).  n_new = 0 and
+ * B = 0 are no-ops.
  * No allocation, no synchronisation; can be captured into a graph.
  */
 typedef struct {

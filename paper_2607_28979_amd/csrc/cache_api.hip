@@ -57,7 +57,7 @@ PageTable page_table(const mot_cache_shapes* c) {
 
 mot_status check_rows(const mot_cache_shapes* c, int n_new, int max_new, bool packed) {
     if (n_new < 0 || max_new < 0) return fail(MOT_ERR_BAD_SHAPE, "n_new=%d max_new=%d must be >= 0", n_new, max_new);
-    if ((int64_t)n_new > 1 << 26) return fail(MOT_ERR_BAD_SHAPE, "n_new=%d exceeds 2^26 tokens", n_new);
+    if (n_new > 4 * kMostWorkgroups) return fail(MOT_ERR_BAD_SHAPE, "n_new=%d exceeds 2^26 - 32 tokens", n_new);
     if (max_new > n_new) return fail(MOT_ERR_BAD_SHAPE, "max_new=%d above n_new=%d", max_new, n_new);
     if (!packed && (int64_t)c->B * max_new != n_new)
         return fail(MOT_ERR_BAD_SHAPE, "n_new=%d is not B * max_new = %d * %d (no new_start)", n_new, c->B, max_new);
@@ -204,6 +204,8 @@ mot_status mot_paged_attention(const void* q, const void* k_pages, const void* v
         if ((st = apart({"workspace", s->workspace, need}, in, 7)) != MOT_OK) return st;
         p.part = reinterpret_cast<float*>(s->workspace);
     }
+    if (!attend_fits(p, c->dtype == MOT_BF16))
+        return fail(MOT_ERR_UNSUPPORTED, "more tiles of query rows than a launch holds (2^24 - 8 workgroups)");
     return launched(launch_paged_attention(p, c->dtype == MOT_BF16, stream));
 }
 

@@ -7,6 +7,8 @@
 
 namespace mot {
 
+constexpr int kMostWorkgroups = (1 << 24) - 8;   // of 256 threads: a launch takes under 2^32 work items
+
 // Pools and page table of one call (element = 2 or 4 bytes).
 struct PageTable {
     const int32_t* table;    // [B][max_pages]
@@ -87,6 +89,8 @@ struct PagesProblem {
 
 // Sets p.n_split, p.least and p.wide; the bytes of `part` that they need (0: nothing is cut).
 size_t attend_plan(AttendProblem& p, bool bf16);
+// Whether every launch of the call is one that a device takes.
+bool attend_fits(const AttendProblem& p, bool bf16);
 hipError_t launch_paged_attention(const AttendProblem& p, bool bf16, hipStream_t stream);
 // bf16 calls on tiles of 32 query rows (k_paged_decode.hip), of 128 (k_paged_chunk.hip), and fp32
 // ones, of 16 (k_paged_f32.hip).  finds: the workgroups find their work, of 512 sequences at most

@@ -42,7 +42,7 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
         store16<PAST>(reinterpret_cast<f32x4*>(p) + i, f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]});
 }
 
-constexpr int kMostTokens = 4;   // tokens of a workgroup
+constexpr int kMostTokens = 4;   // tokens of a workgroup (4 kMostWorkgroups of a call)
 
 // The sequence whose new tokens packed row `row` is among (-1: none), and its number among
 // them, by a wave: the last sequence that starts at `row` or before, 64 starts at a time.
@@ -220,12 +220,14 @@ hipError_t append_as(const AppendProblem& p, hipStream_t stream) {
     const int64_t tokens = (int64_t)p.c.n_new * p.L;
     const int lanes = p.c.D >> 4, lpr = lanes <= 2 ? 2 : lanes <= 4 ? 4 : lanes <= 8 ? 8 : 16;
     const int heads = (p.q ? p.H_q : 0) + (p.k ? 2 * p.c.H_kv : 0);
-    const int tpb = tokens < 1792 ? 1 : kMostTokens * heads * lpr <= 256 ? kMostTokens : 2;
     // Packed rows one by one where most of the places that max_new admits are none: 200 single
     // tokens and 1500 of one sequence, 36 heads of 128, 49 -> 9.5 us, 47 and 512 11.8 -> 5.7,
     // 256 single ones with no bound 27 -> 5.2 (4.6 with it: finding the sequence).
     const bool find = p.c.start && (int64_t)p.c.max_new * p.c.B > 2 * (int64_t)p.c.n_new;
-    const dim3 grid(((find ? p.c.n_new : p.c.max_new) + tpb - 1) / tpb, find ? 1 : p.c.B, p.L);
+    const int rows = find ? p.c.n_new : p.c.max_new;
+    // calls of more than 2^25 rows take four for the launch to hold them
+    const int tpb = tokens < 1792 ? 1 : kMostTokens * heads * lpr <= 256 || rows > 2 * kMostWorkgroups ? kMostTokens : 2;
+    const dim3 grid((rows + tpb - 1) / tpb, find ? 1 : p.c.B, p.L);
     // Stores past the caches where what is written is more than attention finds there again:
     // 28 layers of 1501 tokens, 86 MB written, 36.6 -> 28.4 us, 8192 tokens of 36 heads, 75 MB,
     // 36.7 -> 26.7.  Below, the call itself gains little (38 MB 17.5 -> 16.8) and attention

@@ -143,6 +143,9 @@ size_t attend_plan(AttendProblem& p, bool bf16) {
     const int64_t whole = most_workgroups(p, rows) - 1;   // workgroups of the call uncut
     if (rows == 32 ? p.max_kv <= 1024 : rows == 128 ? whole >= 192 || p.max_kv <= 512 + 8 * whole
                                                     : whole >= 512 || p.max_kv <= 512) return 0;
+    // nor are calls whose rows are too many for the joining launch
+    const bool by_row = (int64_t)p.c.max_new * B > 2 * (int64_t)p.c.n_new;
+    if ((int64_t)(by_row ? max(p.c.n_new, p.c.max_new) : p.c.max_new) * p.H_q > kMostWorkgroups) return 0;
     p.n_split = !bf16 || p.c.D == 128 ? 448 : 704;
     const size_t R = (size_t)partial_of(p, rows).R;
     return 2 * p.n_split * R * (p.c.D + 2) * sizeof(float) + (size_t)B * p.c.H_kv * sizeof(int2);
@@ -170,6 +173,14 @@ hipError_t launch_slice(const AttendProblem& p, bool bf16, int rows, bool finds,
 
 }  // namespace
 
+bool attend_fits(const AttendProblem& p, bool bf16) {
+    const int rows = tile_rows(p, bf16);
+    if (!finds_work(p, rows)) return own_tiles(p, rows) <= kMostWorkgroups;
+    AttendProblem s = shared_out(p);
+    s.c.B = min(p.c.B, kMostSeq);
+    return most_workgroups(s, rows) <= kMostWorkgroups;
+}
+
 // Workgroups that find their work add up as many sequences at a time as fit in a wave's
 // lanes; the slices share the workspace, one after the other.  599 single tokens on 300
 // positions and one on 30000: 365 us whole, 138 so.  Where each has a tile of its own, all
@@ -177,7 +188,7 @@ hipError_t launch_slice(const AttendProblem& p, bool bf16, int rows, bool finds,
 hipError_t launch_paged_attention(const AttendProblem& p, bool bf16, hipStream_t stream) {
     const int rows = tile_rows(p, bf16);
     const bool finds = finds_work(p, rows);
-    const int most = finds ? kMostSeq : p.c.B;
+    const int most = finds ? kMostSeq : min(p.c.B, (int)(kMostWorkgroups / own_tiles(p, rows)));
     for (int b0 = 0; b0 < p.c.B; b0 += most) {
         AttendProblem s = p;
         s.c.B = min(p.c.B - b0, most);

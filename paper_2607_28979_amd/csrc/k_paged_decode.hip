@@ -272,7 +272,6 @@ hipError_t launch_d(const AttendProblem& p, bool finds, hipStream_t stream) {
     if (finds) {
         const AttendProblem s = shared_out(p);
         const int64_t grid = most_workgroups(s, 32);
-        if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
         if (p.c.B <= 64 && !p.part && grid <= 256) k_paged_decode<D, 8, 1><<<(unsigned)grid, 512, 0, stream>>>(s);
         else if (p.c.B <= 64) k_paged_decode<D, 4, 1><<<(unsigned)grid, 256, 0, stream>>>(s);
         else k_paged_decode<D, 4, kSeqPerLane><<<(unsigned)grid, 256, 0, stream>>>(s);

@@ -248,7 +248,6 @@ hipError_t launch_d(const AttendProblem& p, bool finds, hipStream_t stream) {
     const int tiles = div_up(p.c.max_new * (p.H_q / p.c.H_kv), 16);
     const AttendProblem s = shared_out(p);
     const int64_t grid = ((finds ? most_workgroups(s, 16) : (int64_t)p.c.B * p.c.H_kv * tiles) + 7) / 8 * 8;
-    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
     if (!finds) k_paged_f32<D, 0><<<(unsigned)grid, 256, 0, stream>>>(p, tiles);
     else if (p.c.B <= 64) k_paged_f32<D, 1><<<(unsigned)grid, 256, 0, stream>>>(s, tiles);
     else k_paged_f32<D, kSeqPerLane><<<(unsigned)grid, 256, 0, stream>>>(s, tiles);

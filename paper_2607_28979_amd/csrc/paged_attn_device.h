@@ -383,17 +383,22 @@ inline AttendProblem shared_out(AttendProblem p) {
     return p;
 }
 
+// Tiles that own_work() has for a sequence.
+inline int64_t own_tiles(const AttendProblem& p, int rows) {
+    return ((int64_t)p.c.max_new * (p.H_q / p.c.H_kv) + rows - 1) / rows * p.c.H_kv;
+}
+
 // Whether the workgroups of a call of tiles of `rows` rows find their work (shared_work()):
 // where it is cut; where decoding has several tiles to a sequence; and where packed tokens of
 // which one sequence might have most, but has not, would make most of own_work()'s grid leave
 // at once.  47 single tokens and 512 of one sequence, contexts of 1000, 28 heads on 4 of 128:
 // 96 and 36 us; 200 and 1500 on 1500: 316 and 169; fp32, 47 and 100 on 1000: 81 and 42.
 inline bool finds_work(const AttendProblem& p, int rows) {
-    const int64_t tiles = ((int64_t)p.c.max_new * (p.H_q / p.c.H_kv) + rows - 1) / rows;
-    if (p.part || rows == 32) return p.part || tiles > 1;
+    const int64_t tiles = own_tiles(p, rows);
+    if (p.part || rows == 32) return p.part || tiles > p.c.H_kv;
     AttendProblem s = shared_out(p);
     s.c.B = p.c.B < kMostSeq ? p.c.B : kMostSeq;
-    return s.c.B * p.c.H_kv * tiles > 4 * most_workgroups(s, rows);
+    return s.c.B * tiles > 4 * most_workgroups(s, rows);
 }
 
 }  // namespace mot

@@ -285,3 +285,34 @@ def test_long_contexts_are_cut_whatever_the_table_holds(lib, B, n_new, max_new, 
     s = mb._AttendShapes(n_new, max_new, H_q, 0, 0, 0.0, _rows(H_q, D, n_new), _rows(H_q, D, n_new))
     need = lib.mot_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(s))
     assert (0 < need < 1 << 30) if cut else need == 0
+
+
+@pytest.mark.parametrize("cache,kw", [
+    (dict(dtype=mb.MOT_F32, B=1, H_kv=16), dict(n_new=1 << 24, max_new=1 << 24, H_q=16)),
+    (dict(dtype=mb.MOT_F32, B=1, H_kv=16, max_pages=4096), dict(n_new=1 << 24, max_new=1 << 24, H_q=16)),
+    (dict(B=64, H_kv=64), dict(n_new=4 * ((1 << 24) - 8), max_new=1 << 24, H_q=64, packed=True))])
+def test_attention_refuses_what_no_launch_holds(lib, cache, kw):
+    """More workgroups than a launch takes are found before anything is launched."""
+    kw = dict(kw)
+    packed = kw.pop("packed", False)
+    far = {n: FAKE + i * (1 << 41) for i, n in enumerate(("q", "k", "v", "table", "kv_len", "start", "o"))}
+    if not packed:
+        far["start"] = None
+    assert _attend(cache=_cache(**cache), ptrs=far, **kw) == "MOT_ERR_UNSUPPORTED"
+
+
+def test_tokens_of_a_call(lib):
+    for n in (4 * ((1 << 24) - 8) + 1, 1 << 26):
+        for call in (_append, _attend):
+            assert call(cache=_cache(B=1), n_new=n, max_new=n) == "MOT_ERR_BAD_SHAPE"
+            assert b"2^26" in lib.mot_last_error()
+
+
+def test_no_cut_that_no_launch_joins(lib):
+    """Where the partial sums' rows are more than a launch holds, nothing is cut."""
+    c = _cache(B=3, H_kv=1024, max_pages=2048)
+    sizes = lambda n, G: mb._AttendShapes(n, n, 1024 * G, 0, 0, 0.0, _rows(1024 * G, 64, n), _rows(1024 * G, 64, n))  # noqa: E731
+    need = lambda *a: lib.mot_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(sizes(*a)))  # noqa: E731
+    assert need(16, 2) > 0      # 3 sequences, 16 x 2048 rows
+    c = _cache(B=65535, H_kv=1024, max_pages=2048)
+    assert need(65535, 1) == 0 and need(16, 1) > 0

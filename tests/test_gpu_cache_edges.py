@@ -186,3 +186,42 @@ def test_many_short_sequences_are_one_launch(t, B, n, D):
     few = SimpleNamespace(k=c.k, v=c.v, layout=0, host=c.host, table=c.table[pick[some]], kv=[c.kv[i] for i in pick[some]],
                           d_table=table[some].contiguous(), d_kv=kv[some].contiguous())
     assert torch.equal(_attend(few, q[some].contiguous()), o[some])
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_append_of_more_tokens_than_two_to_a_workgroup(packed):
+    """2^25 new tokens and some, of one narrow head: more than 2^24 workgroups of two tokens."""
+    import torch
+    n, ps = (1 << 25) + 37, 1024
+    pages = -(-n // ps)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    print("case far append", packed, flush=True)
+    x = torch.randint(-9, 9, (n, 2, 16), generator=g, device="cuda", dtype=torch.int8).bfloat16()
+    kp, vp = (torch.full((pages + 2, ps, 1, 16), KEEP, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    order = torch.randperm(pages + 2, generator=g, device="cuda")[:pages].int()
+    table = torch.full((3 if packed else 1, pages), -1, dtype=torch.int32, device="cuda")
+    table[-1] = order
+    k, v = x[:, :1], x[:, 1:]
+    if packed:      # no bound, two sequences of none before the one
+        mb.cache_append(None, k, v, None, kp, vp, table, _i32([0, 0, n]), new_start=_i32([0, 0, 0, n]))
+    else:
+        mb.cache_append(None, k[None], v[None], None, kp, vp, table, _i32([n]))
+    for pool, y in ((kp, k), (vp, v)):
+        assert torch.equal(pool[order.long()].reshape(-1, 1, 16)[:n], y)
+        assert int((pool == KEEP).all(-1).sum()) == (pages + 2) * ps - n
+
+
+def test_append_of_more_rows_than_two_tokens_to_a_workgroup_hold():
+    """The same number of queries of 33 heads, whose workgroups take two tokens elsewhere, normed in place:
+    rows of twos become the gain exactly (16 of 4 are 64, the mean's root 2, with eps 0)."""
+    import torch
+    n = (1 << 25) + 37
+    print("case far queries", flush=True)
+    q = torch.full((1, n, 33, 16), 2.0, dtype=torch.bfloat16, device="cuda")
+    gain = torch.arange(-8, 8, device="cuda").bfloat16()
+    pool = torch.zeros((1, 16, 1, 16), dtype=torch.bfloat16, device="cuda")
+    mb.cache_append(q, None, None, q, pool, pool.clone(), _i32([[0]]), _i32([7]), q_gain=gain, eps=0.0)
+    for at in range(0, n, 1 << 21):
+        assert (q[0, at:at + (1 << 21)] == gain).all()
+    del q
+    torch.cuda.empty_cache()
