@@ -171,11 +171,13 @@ __device__ __forceinline__ float add_bf16x2(uint32_t w, float l) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(two, w), __builtin_bit_cast(two, 0x3f803f80u), l, false);
 }
 
-// Two probabilities as two bf16 terms each (x: rounded, y: the rounded remainders), off by 2^-16
-// of themselves at most.
+// Two probabilities as two bf16 terms each, x: cut to 8 bits from just below, y: the rounded
+// rest, off by 2^-15 of them at most.  Neither term of a probability above 0 is 0 or
+// negative, so that an infinite value times it stays what it is.
 __device__ __forceinline__ u32x2 split_bf16x2(float a, float b) {
-    const uint32_t hi = pack_bf16x2(a, b);
-    return {hi, pack_bf16x2(a - bf16_lo(hi), b - bf16_hi(hi))};
+    const uint32_t x = __builtin_elementwise_sub_sat(__float_as_uint(a), 1u) & 0xffff0000u;
+    const uint32_t y = __builtin_elementwise_sub_sat(__float_as_uint(b), 1u) & 0xffff0000u;
+    return {x >> 16 | y, pack_bf16x2(a - __uint_as_float(x), b - __uint_as_float(y))};
 }
 
 // Running softmax of a row: `mo` is the largest exponent so far (base 2), -inf

@@ -22,9 +22,9 @@ pytestmark = pytest.mark.gpu
     ([60, 33, 200], 1, 28, 4, 128, False), ([1500, 90], 1, 12, 2, 128, True), ([150, 77], 4, 14, 2, 64, False),
     ([100, 300, 40], [3, 10, 0], 14, 2, 64, False), ([100, 300, 40], [3, 11, 0], 14, 2, 64, False), ([2000] + [50] * 7, [40] + [1] * 7, 8, 2, 64, True)])
 def test_probabilities_of_few_rows(kv, new, Hq, H, D, cut):
-    """Tiles of 32 rows: a probability is off by 2^-16 of itself at most (two bf16 terms, the second's
-    rounding 2^-8 of at most 2^-8), so the result by 2^-16 of sum of softmax |v| beside its own rounding and
-    the fp32 steps.  14 tokens of 7 query heads are 98 rows, more than the 32 of each of 3 sequences: those
+    """Tiles of 32 rows: a probability is off by 2^-15 of itself at most (two bf16 terms, the first cut to 8
+    bits, 2^-7 of it at most, the second's rounding 2^-8 of that), so the result by 2^-15 of sum of
+    softmax |v| beside its own rounding and the fp32 steps.  14 tokens of 7 query heads are 98 rows, more than the 32 of each of 3 sequences: those
     probabilities are rounded once, and the bound is that of tiles of 128 rows."""
     import torch
     rng = np.random.default_rng(sum(kv))
@@ -41,7 +41,7 @@ def test_probabilities_of_few_rows(kv, new, Hq, H, D, cut):
     most = flat[0] if packed else new
     few = most * (Hq // H) <= 32 or flat[0] * (Hq // H) <= 32 * len(kv)
     assert few == (new != [3, 11, 0])
-    bound = HALF["bf16"] * np.abs(want) + mag * (2.0 ** -16 + (2 * (D + 4) * smax + 2 * (max(kv) + 8)) * 2.0 ** -24) + 1e-30
+    bound = HALF["bf16"] * np.abs(want) + mag * (2.0 ** -15 + (2 * (D + 4) * smax + 2 * (max(kv) + 8)) * 2.0 ** -24) + 1e-30
     if not few:
         bound = _bound("bf16", want, mag, smax, D, max(kv), True)
     bad = ~(np.abs(_np(o).reshape(flat) - want) <= bound)
@@ -225,3 +225,72 @@ def test_append_of_more_rows_than_two_tokens_to_a_workgroup_hold():
         assert (q[0, at:at + (1 << 21)] == gain).all()
     del q
     torch.cuda.empty_cache()
+
+
+def _poisoned(c, q, counts, window, places):
+    """The call's result where (pool, sequence, position, KV head, element, value) are put into the cache: non-finite
+    results exactly where and what the definition says, the others within the bound."""
+    import torch
+    t = "bf16" if q.dtype == torch.bfloat16 else "f32"
+    H, D = q.shape[-2:]
+    n = q.shape[0] if counts is not None else q.shape[1]
+    start = None if counts is None else np.concatenate([[0], np.cumsum(counts)])
+    for pool, b, pos, h, d, x in places:
+        getattr(c, pool)[c.table[b, pos // c.ps], pos % c.ps, h, d] = x
+    outs = []
+    for scratch in (None, False):
+        o = torch.full_like(q, KEEP)
+        mb.paged_attention(q, c.k, c.v, c.d_table, c.d_kv, o, new_start=None if start is None else _i32(start), window=window,
+                           scratch=scratch)
+        torch.cuda.synchronize()
+        outs.append(_np(o).reshape(-1, H, D))
+    k, v = c.host()
+    flat = np.full(outs[0].shape, KEEP)
+    rows = _np(q).reshape(flat.shape)
+    with np.errstate(invalid="ignore"):
+        want, mag, _ = ref.paged_attention(rows, k, v, c.table, c.kv, flat, start, n, window)
+    fine = np.where(np.isfinite(k), k, 0.0)
+    smax = ref.paged_attention(rows, fine, np.nan_to_num(v), c.table, c.kv, flat, start, n, window)[2]
+    G = H // c.k.shape[2]
+    bound = _bound(t, want, mag, smax, D, max(c.kv), t == "bf16" and n * G > 32)
+    for got in outs:
+        with np.errstate(invalid="ignore"):
+            bad = ~((np.abs(got - want) <= bound) & np.isfinite(want)) & (got != want) & ~(np.isnan(got) & np.isnan(want))
+        worst = np.unravel_index(np.argmax(bad), bad.shape)
+        assert not bad.any(), (int(bad.sum()), worst, got[worst], want[worst], bound[worst])
+    return want
+
+
+@pytest.mark.parametrize("t,n,H,G,D", [("bf16", 1, 2, 6, 128), ("bf16", 1, 2, 7, 64), ("bf16", 3, 2, 4, 128), ("bf16", 40, 2, 4, 64),
+                                       ("bf16", 40, 2, 6, 128), ("f32", 1, 2, 6, 64), ("f32", 9, 2, 2, 128), ("f32", 40, 2, 2, 64)])
+@pytest.mark.parametrize("window", [0, 1300])
+def test_values_that_are_not_finite_in_cut_contexts(t, n, H, G, D, window):
+    """NaN and infinite values and keys in the first, a middle and the last part of contexts that are
+    cut, some of which only later tokens see or, with a window, only earlier ones."""
+    import torch
+    print("case poison", t, n, D, window, flush=True)
+    for seed in range(3):
+        rng = np.random.default_rng(100 * n + seed)
+        kv = [2900, 1500, 700 + 3 * n, 40]
+        c = Cache(rng, kv, 16, H, D, t, max_pages=1024)
+        q, _ = _rand(rng, (len(kv), n, H * G, D), t)
+        inf, nan = float("inf"), float("nan")
+        low = kv[0] - n - 1300 + 1 + (n > 1)               # the window's low end of the first (or second) token
+        places = [[("v", 0, 5, 1, 3, nan), ("v", 1, 1499, 0, 7, -inf)],                     # first part; last position
+                  [("v", 0, 1700, 1, 0, inf), ("k", 1, 1500 - n, 0, 1, nan), ("v", 2, 300, 1, 2, inf)],
+                  [("v", 0, low, 0, 9, inf), ("v", 1, 1500 - (n + 1) // 2, 1, 4, nan), ("k", 2, 690, 0, 0, nan)]][seed]
+        want = _poisoned(c, q, None, window, places)
+        assert (~np.isfinite(want)).any() and np.isfinite(want).any()
+
+
+@pytest.mark.parametrize("t,n,G", [("bf16", 1, 6), ("bf16", 40, 4), ("f32", 9, 2)])
+def test_infinite_keys(t, n, G):
+    """A key of infinity: its position has all the weight, which is no number, or none of it, by the
+    sign of the query's element."""
+    print("case infinite keys", t, n, flush=True)
+    rng = np.random.default_rng(n)
+    for kv, M in (([90, 50], 6), ([2000, 900], 1024)):
+        c = Cache(rng, kv, 16, 2, 64, t, max_pages=M)
+        q, _ = _rand(rng, (2, n, 2 * G, 64), t)
+        want = _poisoned(c, q, None, 0, [("k", 0, 20, 1, 3, float("inf")), ("k", 1, kv[1] - 1, 0, 5, -float("inf"))])
+        assert np.isnan(want).any() and np.isfinite(want).any()
