@@ -500,7 +500,8 @@ typedef struct {
  * are few: max_new H_q / H_kv at most 32, or n_new H_q / H_kv at most 32 B;
  * elsewhere rounded to bf16, as replay attention does.
  * Positions from kv_len on and holes are not looked at, whatever they hold;
- * a NaN or infinite value reaches the tokens that see it and no others.
+ * a NaN or infinite value reaches the tokens that see it and no others.  A row
+ * that sees positions, all with the score -inf, is NaN.
  *
  *   q, o         device, dtype: rows of the new tokens, strides below (head
  *                pitch and all); o must not overlap q, the pools or the tables

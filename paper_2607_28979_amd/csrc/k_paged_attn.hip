@@ -75,7 +75,7 @@ __device__ __forceinline__ void join_row(const AttendProblem& p, int rows, int b
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] += wt * z[j];
     }
-    const float inv = l != 0.f ? 1.0f / l : 0.f;
+    const float inv = inverse_of(M, l);
     T* o = reinterpret_cast<T*>(p.o) + row_offset(p.c, p.os, nt, b, t) + h * p.os.head + 4 * c;
     if constexpr (sizeof(T) == 2)
         *reinterpret_cast<u32x2*>(o) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};

@@ -94,6 +94,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
         float mo = -INFINITY, l = 0.f;
+        bool seen = false;   // some position by this lane's row
         Groups gr;
         gr.base = 0; gr.page = -1; gr.ok = 0;
         auto issue = [&](int kc, int st) {
@@ -171,8 +172,12 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const int v = kc + kb * 32 + 8 * (e >> 2) + 4 * g + (e & 3);
-                            sc[kb][e] = v <= u && v >= ulo && v >= lo && v < hi && ((ok >> (2 * kb + (e >> 3))) & 1u) ? sc[kb][e] : -INFINITY;
+                            const bool see = v <= u && v >= ulo && v >= lo && v < hi && ((ok >> (2 * kb + (e >> 3))) & 1u);
+                            seen |= see;
+                            sc[kb][e] = see ? sc[kb][e] : -INFINITY;
                         }
+                } else {
+                    seen = true;
                 }
                 float cm = -INFINITY;
 #pragma unroll
@@ -216,6 +221,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
             barrier();   // the next chunk has landed; every wave is done with this one
         }
         l += __shfl_xor(l, 32, 64);
+        if (mo == -INFINITY && (seen | __shfl_xor((int)seen, 32, 64))) mo = kLowest;
         if (!exact) {
             float t = 0.f;   // NaN where an accumulator is not finite
 #pragma unroll
@@ -239,7 +245,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
                             f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]};
                 if (g == 0) pt.ml[row] = make_float2(mo, l);
             } else {
-                const float inv = l != 0.f ? 1.0f / l : 0.f;
+                const float inv = inverse_of(mo, l);
                 uint16_t* o = reinterpret_cast<uint16_t*>(p.o) + row_offset(p.c, p.os, nt, b, tok) + head * p.os.head;
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db)

@@ -184,6 +184,13 @@ __device__ __forceinline__ u32x2 split_bf16x2(float a, float b) {
 // before the first visible position; `base` replaces it where it is -inf.
 __device__ __forceinline__ float base_of(float mo) { return mo == -INFINITY ? 0.f : mo; }
 
+// The base of a row that sees positions, all with the score -inf (infinite keys): any other's is above
+// it, so it adds nothing to what other waves or parts of the row have seen.
+constexpr float kLowest = -3.4028234663852886e38f;
+// What a row's accumulators are divided by: nothing seen gives zeros, a softmax of -inf alone
+// is no number.
+__device__ __forceinline__ float inverse_of(float mo, float l) { return l != 0.f ? 1.0f / l : mo == -INFINITY ? 0.f : NAN; }
+
 // ---- sharing the work --------------------------------------------------------
 //
 // Lengths differ within a batch, and only the device knows them.  With few tiles and

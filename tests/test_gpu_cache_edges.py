@@ -294,3 +294,27 @@ def test_infinite_keys(t, n, G):
         q, _ = _rand(rng, (2, n, 2 * G, 64), t)
         want = _poisoned(c, q, None, 0, [("k", 0, 20, 1, 3, float("inf")), ("k", 1, kv[1] - 1, 0, 5, -float("inf"))])
         assert np.isnan(want).any() and np.isfinite(want).any()
+
+
+@pytest.mark.parametrize("t,n,G,D", [("bf16", 1, 6, 128), ("bf16", 3, 4, 64), ("bf16", 40, 4, 64), ("bf16", 40, 4, 128), ("f32", 9, 2, 64),
+                                     ("f32", 20, 2, 128)])
+@pytest.mark.parametrize("window", [0, 600])
+def test_scores_of_minus_infinity_alone(t, n, G, D, window):
+    """Rows all of whose positions have the score -inf have no softmax: NaN, not the zeros of a row that
+    sees no position.  Rows that see one other position as well have that one's value."""
+    import torch
+    print("case minus", t, n, D, window, flush=True)
+    rng = np.random.default_rng(n + D)
+    for kv, M in (([90, 50, n - 1, 33], 8), ([2000, 900, n - 1, 700], 1024)):
+        c = Cache(rng, kv, 16, 2, D, t, max_pages=M)
+        q = _rand(rng, (4, n, 2 * G, D), t)[0]
+        q[..., 0].abs_()
+        for b in (0, 1, 3):                         # KV head 0 of these: nothing but -inf ...
+            for j in range(c.kv[b]):
+                c.k[c.table[b, j // 16], j % 16, 0, 0] = -float("inf")
+        for b, j in ((1, kv[1] - 1), (3, 20)):      # ... but for a position
+            c.k[c.table[b, j // 16], j % 16, 0, 0] = 1.0
+        want = _poisoned(c, q, None, window, [])
+        want = want.reshape(4, n, 2, G, D)
+        assert np.isnan(want[0, :, 0]).all() and np.isfinite(want[1, -1]).all() and np.isfinite(want[:, :, 1]).all()
+        assert (want[2, 0] == 0).all() and np.isnan(want[1, :-1, 0]).all()
