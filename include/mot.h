@@ -514,7 +514,7 @@ typedef struct {
  *   max_kv       0, or a bound on kv_len that is better than max_pages *
  *                page_size (a hint for how work is cut; longer sequences are
  *                still attended in full)
- *   scale        0: 1 / sqrt(D); positive
+ *   scale        0: 1 / sqrt(D); positive, scale log2(e) finite in fp32
  *   q, o strides of q and o (layer not used)
  *   workspace, workspace_bytes
  *                optional device scratch of this call (16-byte aligned, not

@@ -119,6 +119,11 @@ mot_status apart(const Extent& out, const Extent* others, int n) {
     return MOT_OK;
 }
 
+// scale * log2(e)
+float scale_log2(const mot_cache_shapes* c, const mot_attend_shapes* s) {
+    return (float)((s->scale > 0.f ? (double)s->scale : 1.0 / sqrt((double)c->D)) * 1.4426950408889634);
+}
+
 mot_status check_attend(const mot_cache_shapes* c, const mot_attend_shapes* s, bool packed) {
     mot_status st = check_cache(c);
     if (st != MOT_OK) return st;
@@ -132,7 +137,9 @@ mot_status check_attend(const mot_cache_shapes* c, const mot_attend_shapes* s, b
         return fail(MOT_ERR_BAD_SHAPE, "max_new=%d: more than 2^30 query rows of a sequence", s->max_new);
     if (s->window < 0 || s->max_kv < 0)
         return fail(MOT_ERR_BAD_SHAPE, "window=%d max_kv=%d must be >= 0", s->window, s->max_kv);
-    if (!(s->scale >= 0.f) || isinf(s->scale)) return fail(MOT_ERR_BAD_SHAPE, "scale must be positive (0: 1 / sqrt(D))");
+    // 0 * infinity would make rows of zeros NaN
+    if (!(s->scale >= 0.f) || isinf(scale_log2(c, s)))
+        return fail(MOT_ERR_BAD_SHAPE, "scale must be positive (0: 1 / sqrt(D)), scale * log2(e) a finite float");
     if (c->D != 64 && c->D != 128)
         return fail(MOT_ERR_UNSUPPORTED, "D=%d: paged attention supports head dims 64 and 128", c->D);
     return MOT_OK;
@@ -149,7 +156,7 @@ AttendProblem attend_problem(const mot_cache_shapes* c, const mot_attend_shapes*
     // lie at -2^26 or later, so u - window fits in 32 bits.
     p.window = s->window < most ? s->window : 0;
     p.max_kv = s->max_kv > 0 && s->max_kv < most ? s->max_kv : most;
-    p.scale_log2 = (float)((s->scale > 0.f ? (double)s->scale : 1.0 / sqrt((double)c->D)) * 1.4426950408889634);
+    p.scale_log2 = scale_log2(c, s);
     p.qs = strides(s->q);
     p.os = strides(s->o);
     return p;

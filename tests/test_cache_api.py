@@ -316,3 +316,10 @@ def test_no_cut_that_no_launch_joins(lib):
     assert need(16, 2) > 0      # 3 sequences, 16 x 2048 rows
     c = _cache(B=65535, H_kv=1024, max_pages=2048)
     assert need(65535, 1) == 0 and need(16, 1) > 0
+
+
+@pytest.mark.parametrize("scale", [3.0e38, 2.4e38])
+def test_attention_refuses_scales_past_fp32(lib, scale):
+    """scale * log2(e) is what scores are multiplied by: from 2.36e38 on it is infinite, and rows of
+    zeros would be NaN."""
+    assert _attend(scale=scale) == "MOT_ERR_BAD_SHAPE"
