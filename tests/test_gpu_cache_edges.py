@@ -13,7 +13,7 @@ import pytest
 from oracle import cache as ref
 from paper_2607_28979_amd import binding as mb
 
-from test_gpu_cache import HALF, KEEP, Cache, _attend, _bound, _i32, _np, _rand
+from test_gpu_cache import HALF, KEEP, Cache, _attend, _bound, _dt, _i32, _np, _rand
 
 pytestmark = pytest.mark.gpu
 
@@ -318,3 +318,52 @@ def test_scores_of_minus_infinity_alone(t, n, G, D, window):
         want = want.reshape(4, n, 2, G, D)
         assert np.isnan(want[0, :, 0]).all() and np.isfinite(want[1, -1]).all() and np.isfinite(want[:, :, 1]).all()
         assert (want[2, 0] == 0).all() and np.isnan(want[1, :-1, 0]).all()
+
+
+@pytest.mark.parametrize("which,dst_layout,page_layout", [(0, 0, 0), (0, 1, 1), (1, 0, 1), (1, 1, 0), (2, 0, 0), (3, 1, 0)])
+def test_answering_from_a_translated_context(which, dst_layout, page_layout):
+    """A context translated by mot_translate, stored into pages as it lies (every layer at once), then a
+    prompt and single tokens over it, call after call on one stream: the pages hold the translated rows
+    bit for bit and every layer's attention is the oracle's over them."""
+    import torch
+    from paper_2607_28979_amd.configs import WORKLOADS, small_variant
+    from paper_2607_28979_amd.inputs import generate
+    from helpers import dst_shape, to_dev
+    w = small_variant(WORKLOADS[which], L_src=2, L_tgt=3, B=2, T=70).with_(dst_layout=dst_layout)
+    t, B, T, H, D, ps = w.dtype, w.B, w.T, w.H_tgt, w.D_tgt, 16
+    print("case translated", w.name, dst_layout, page_layout, flush=True)
+    inp = generate(w)
+    dev = {n: to_dev(getattr(inp, n), t) for n in ("src_k", "src_v", "w1", "b1", "w2", "b2", "wr", "br")}
+    dk, dv = (torch.empty(dst_shape(w), dtype=_dt(t), device="cuda") for _ in range(2))
+    L, G, M = w.L_tgt, 3, 8
+    rng = np.random.default_rng(which)
+    table = _i32(rng.permutation(B * M + 3)[:B * M].reshape(B, M))
+    shape = (L, B * M + 3) + ((H, ps, D) if page_layout else (ps, H, D))
+    k, v = (torch.full(shape, float("nan"), dtype=_dt(t), device="cuda") for _ in range(2))
+    f = torch.rand(D // 2, device="cuda")
+    mb.translate(dev["src_k"], dev["src_v"], mb.depth_ratio_map(w.L_src, L), dev["w1"], dev["b1"], dev["w2"], dev["b2"], dev["wr"],
+                 dev["br"], dk, dv, mb.Shapes.from_workload(w))
+    rows = [x.transpose(2, 3) if dst_layout else x for x in (dk, dv)]          # [L][B][T][H][D]
+    mb.cache_append(None, *rows, None, k, v, table, _i32([T] * B), page_layout=page_layout)
+    steps = []
+    for n, kv in ((9, T + 9), (1, T + 10), (1, T + 11)):
+        fused = _rand(rng, (L, B, n, G * H + 2 * H, D), t)[0]
+        q = torch.empty((L, B, n, G * H, D), dtype=_dt(t), device="cuda")
+        mb.cache_append(fused[..., :G * H, :], fused[..., G * H:G * H + H, :], fused[..., G * H + H:, :], q, k, v, table, _i32([kv] * B),
+                        inv_freq=f, page_layout=page_layout)
+        o = torch.full_like(q, KEEP)
+        for l in range(L):
+            mb.paged_attention(q[l], k[l], v[l], table, _i32([kv] * B), o[l], page_layout=page_layout)
+        steps.append((n, kv, q, o))
+    torch.cuda.synchronize()
+    for pool, x in ((k, rows[0]), (v, rows[1])):
+        held = pool[:, table.long()]                                            # [L][B][M] x page
+        held = (held.transpose(3, 4) if page_layout else held).reshape(L, B, M * ps, H, D)
+        assert torch.isfinite(x).all() and torch.equal(held[:, :, :T], x)
+        assert torch.isfinite(held[:, :, :T + 11]).all() and torch.isnan(held[:, :, T + 11:]).all()
+    for n, kv, q, o in steps:
+        for l in range(L):
+            flat = _np(q[l]).reshape(B * n, G * H, D)
+            want, mag, smax = ref.paged_attention(flat, _np(k[l]), _np(v[l]), table.cpu().numpy(), [kv] * B, flat, max_new=n,
+                                                  layout=page_layout)
+            assert (np.abs(_np(o[l]).reshape(want.shape) - want) <= _bound(t, want, mag, smax, D, kv)).all(), (n, l)
