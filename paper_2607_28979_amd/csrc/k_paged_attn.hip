@@ -110,8 +110,8 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendProblem p, int rows, b
 
 // Rows of a tile: 32 where all of a sequence's fit, or an average one's do (packed tokens
 // with a loose max_new), else 128; fp32 16.  With no max_new, 128 and 32 rows: 48 single
-// tokens on 4000 114 and 86 us, 256 on 300 66 and 42, 32 x 4 on 2000 118 and 41, 47 and 100 of
-// one sequence on 4000 116 and 102.
+// tokens on 4000 114 and 89 us, 256 on 300 41 and 38, 32 x 4 on 2000 40 and 39, 47 and 100 of
+// one sequence on 4000 101 and 106.
 int tile_rows(const AttendProblem& p, bool bf16) {
     const int64_t G = p.H_q / p.c.H_kv;
     return !bf16 ? 16 : p.c.max_new * G <= 32 || p.c.n_new * G <= 32 * (int64_t)p.c.B ? 32 : 128;
@@ -122,16 +122,19 @@ int tile_rows(const AttendProblem& p, bool bf16) {
 // When positions are cut, and over how many workgroups.  Cutting costs a second launch and
 // 4 us or so of finding the parts and joining them, more with many rows; it saves
 // the time that a long context takes a few workgroups.  28 heads on 4 of 128 unless said.
-// Few rows, calls back to back, whole against cut: one sequence of 500 positions 9.0 /
-// 12.6 us, 800 10.9 / 12.5, 1100 12.9 / 12.5, 1500 16.5 / 12.4; 32 of 1000 15.9 / 18.8; 48
-// of 205 to 8192 104 / 52 (kernels).  Tiles of 128 rows (kernels): 37 new tokens on 8000
-// 167 / 28 us, 200 on 1000 28.5 / 28.4, 2 x 300 on 700 23 / 47, 2 x 500 alone 20 / 57,
-// 16 x 20 on up to 6000 129 / 36, 1000 on 4000 91 / 120, 2 x 300 on 3000 with 16 heads
-// of 64 51 / 44.  fp32: 12 heads of 64, one token on 1000 19 / 10.2, 3 x 64 on 333 10 /
-// 16, 40 ragged ones on up to 2000 47 / 42; 12 heads on 2 of 128, 500 tokens on 2000 105 / 97.
-// Shares: 7/8 of the workgroups that the chip holds (two per CU at D = 128, three at 64),
-// since remainders add some: 30 ragged contexts on 2 heads 18.6 us with 448, 22.1
-// with 512 to 704.
+// Few rows, calls back to back, whole against cut: one sequence of 500 positions 8.7 /
+// 13.0 us, 800 10.2 / 12.7, 1100 12.3 / 12.9, 1500 15.8 / 12.6; 32 of 1000 15.9 / 20.4; 48
+// of up to 8192 69 / 53.  Tiles of 128 rows (replayed): 37 new tokens on 8000 171 / 29 us,
+// 200 on 1000 29.7 / 28.5, 2 x 300 on 700 24 / 49, 2 x 500 alone 20 / 60, 16 x 20 on up to
+// 6000 130 / 42, 1000 on 4000 93 / 120, 2 x 300 on 3000 with 16 heads of 64 53 / 42.  fp32: 12
+// heads of 64, one token on 1000 19 / 11.2, 3 x 64 on 333 10.6 / 15.4, 40 ragged ones on up to
+// 2000 46 / 44; 12 heads on 2 of 128, 500 tokens on 2000 105 / 97.
+// Shares: 448, 7/8 of the workgroups that the chip holds at two per CU, since remainders add
+// some: 30 ragged contexts on 2 heads 18.6 us with 448, 22.1 with 512 to 704.  bf16 at D = 64,
+// three per CU: 704 of 768 (48 ragged contexts 20.3 us with 672 or 704, 20.0 with 448).  fp32 at
+// D = 128 holds one per CU (131 KB of LDS) and still takes 448, since parts of several tiles
+// do better in two rounds: 500 tokens on 2000 99 us and 3 x 64 on 2000 55, with 224 111 and 65; 40
+// single ones on up to 2000 24.6 and 20.1.
 size_t attend_plan(AttendProblem& p, bool bf16) {
     const int rows = tile_rows(p, bf16), step = rows == 128 ? 64 : 32, B = min(p.c.B, kMostSeq);
     p.n_split = 1;
@@ -183,7 +186,7 @@ bool attend_fits(const AttendProblem& p, bool bf16) {
 
 // Workgroups that find their work add up as many sequences at a time as fit in a wave's
 // lanes; the slices share the workspace, one after the other.  599 single tokens on 300
-// positions and one on 30000: 365 us whole, 138 so.  Where each has a tile of its own, all
+// positions and one on 30000: 396 us whole, 136 so.  Where each has a tile of its own, all
 // sequences are one launch: 4096 single tokens on 100 positions 224 us, in slices 251.
 hipError_t launch_paged_attention(const AttendProblem& p, bool bf16, hipStream_t stream) {
     const int rows = tile_rows(p, bf16);

@@ -94,7 +94,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
         float mo = -INFINITY, l = 0.f;
-        bool seen = false;   // some position by this lane's row
         Groups gr;
         gr.base = 0; gr.page = -1; gr.ok = 0;
         auto issue = [&](int kc, int st) {
@@ -172,12 +171,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const int v = kc + kb * 32 + 8 * (e >> 2) + 4 * g + (e & 3);
-                            const bool see = v <= u && v >= ulo && v >= lo && v < hi && ((ok >> (2 * kb + (e >> 3))) & 1u);
-                            seen |= see;
-                            sc[kb][e] = see ? sc[kb][e] : -INFINITY;
+                            sc[kb][e] = v <= u && v >= ulo && v >= lo && v < hi && ((ok >> (2 * kb + (e >> 3))) & 1u) ? sc[kb][e] : -INFINITY;
                         }
-                } else {
-                    seen = true;
                 }
                 float cm = -INFINITY;
 #pragma unroll
@@ -221,7 +216,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
             barrier();   // the next chunk has landed; every wave is done with this one
         }
         l += __shfl_xor(l, 32, 64);
-        if (mo == -INFINITY && (seen | __shfl_xor((int)seen, 32, 64))) mo = kLowest;
+        if (wave_ok) mo = settled(p, b, mo, u, lo, hi, 0, 1);
         if (!exact) {
             float t = 0.f;   // NaN where an accumulator is not finite
 #pragma unroll
@@ -234,9 +229,12 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
         }
         // lane holds d = 32 db + 8 i + 4 g + {0..3} of its row
         if (row_ok && (!exact || tok == only)) {
+            // opaque, so that addresses are not held through the loop above, which has every register
+            int at = tok, h = head, x = r;
+            asm volatile("" : "+v"(at), "+v"(h), "+v"(x));
             if (cut) {
                 const Partial pt = partial_of(p, 128);
-                const int64_t row = partial_row(pt, wk) + r - tl.r0;
+                const int64_t row = partial_row(pt, wk) + x - tl.r0;
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -246,7 +244,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendProblem p, int til
                 if (g == 0) pt.ml[row] = make_float2(mo, l);
             } else {
                 const float inv = inverse_of(mo, l);
-                uint16_t* o = reinterpret_cast<uint16_t*>(p.o) + row_offset(p.c, p.os, nt, b, tok) + head * p.os.head;
+                uint16_t* o = reinterpret_cast<uint16_t*>(p.o) + row_offset(p.c, p.os, nt, b, at) + h * p.os.head;
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db)
 #pragma unroll

@@ -95,7 +95,6 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
         float mo = -INFINITY, l = 0.f;
-        bool seen = false;   // some position by this lane's row
         GroupRows rows[2];   // of the block loaded last
         auto load = [&](int kb, const void* pool, const uint32_t (&off)[NL], u32x4* tile) {
             const rsrc_t r0 = group_rsrc<uint16_t>(pool, rows[0]), r1 = group_rsrc<uint16_t>(pool, rows[1]);
@@ -148,12 +147,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int v = kb + 8 * (e >> 2) + 4 * g + (e & 3);
-                    const bool see = v <= u && v >= ulo && v >= lo && v < hi && ((okb >> (e >> 3)) & 1u);
-                    seen |= see;
-                    sc[e] = see ? sc[e] : -INFINITY;
+                    sc[e] = v <= u && v >= ulo && v >= lo && v < hi && ((okb >> (e >> 3)) & 1u) ? sc[e] : -INFINITY;
                 }
-            } else {
-                seen = true;
             }
             float cm = sc[0];
 #pragma unroll
@@ -202,7 +197,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_decode(AttendProblem p) {
             step(Step<1>{});
             if (more) load_v(nx);   // the V operands are read
         }
-        if (mo == -INFINITY && (seen | __shfl_xor((int)seen, 32, 64))) mo = kLowest;
+        mo = settled(p, b, mo, u, lo, hi, w, NW);
         // the waves' rows, joined through their tiles: row, chunk c of four floats at c ^ (row % (D / 4))
         f32x4* mine = reinterpret_cast<f32x4*>(Kt);
 #pragma unroll

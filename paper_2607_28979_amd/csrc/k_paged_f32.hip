@@ -76,7 +76,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_f32(AttendProblem p, int tiles
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
         float mo = -INFINITY, l = 0.f;
-        bool seen = false;   // some position by this lane's row
         Groups gr;
         gr.base = 0; gr.page = -1; gr.ok = 0;
         GroupRows rows[2];   // of the block loaded last
@@ -136,9 +135,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_f32(AttendProblem p, int tiles
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int v = kb + 16 * h + 4 * g4 + j;
-                    const bool see = v <= u && v >= ulo && v >= lo && v < hi && ((ok >> h) & 1u);
-                    seen |= see;
-                    sc[h][j] = see ? sc[h][j] : -INFINITY;
+                    sc[h][j] = v <= u && v >= ulo && v >= lo && v < hi && ((ok >> h) & 1u) ? sc[h][j] : -INFINITY;
                     cm = fmaxf(cm, sc[h][j]);
                 }
             cm = fmaxf(cm, __shfl_xor(cm, 16, 64));
@@ -180,9 +177,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_f32(AttendProblem p, int tiles
             wave_lds_sync();   // the V operands are read: the next V may land
             if (more) load(nx, p.v, voff, Vt);
         }
-        int any = seen | __shfl_xor((int)seen, 16, 64);
-        any |= __shfl_xor(any, 32, 64);
-        if (mo == -INFINITY && any) mo = kLowest;
+        mo = settled(p, b, mo, u, lo, hi, w, NW);
         // the waves' rows, joined through their tiles: row, chunk c of four floats at c ^ row
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) Kt[l16 * DC + ((4 * db + g4) ^ l16)] = acc[db];

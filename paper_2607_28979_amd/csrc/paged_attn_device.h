@@ -187,6 +187,26 @@ __device__ __forceinline__ float base_of(float mo) { return mo == -INFINITY ? 0.
 // The base of a row that sees positions, all with the score -inf (infinite keys): any other's is above
 // it, so it adds nothing to what other waves or parts of the row have seen.
 constexpr float kLowest = -3.4028234663852886e38f;
+// The base of this lane's row (token at position u of sequence b) once a wave's positions are done: blocks
+// of 32 of [lo, hi), the w-th and every nw-th after it (nw = 1: all).  By a whole wave; the pages are
+// looked at again only where no score of a row that lies behind one of them was above -inf.
+__device__ __forceinline__ float settled(const AttendProblem& p, int b, float mo, int u, int lo, int hi, int w, int nw) {
+    if (!__builtin_amdgcn_ballot_w64(mo == -INFINITY)) return mo;   // uniform
+    const int a = max(low_of(p, u), lo), e = min(u + 1, hi);        // seen, as far as no hole covers it
+    // the wave's first block that holds a or lies behind it
+    const int j = a >> 5, first = 32 * (j + ((w - j + (lo >> 5)) & (nw - 1)));
+    const bool none = mo == -INFINITY && a < e && first < e;
+    if (!__builtin_amdgcn_ballot_w64(none)) return mo;
+    bool seen = false;
+    for (int g = lo >> 4; (g << 4) < hi; g += 64) {
+        Groups gr;
+        gr.load(p, b, g);
+        const int from = max((a >> 4) - g, 0), to = min(((e + 15) >> 4) - g, 64);
+        if (from < to) seen |= (gr.ok >> from & ~0ull >> (64 - (to - from))) != 0;
+    }
+    return none && seen ? kLowest : mo;
+}
+
 // What a row's accumulators are divided by: nothing seen gives zeros, a softmax of -inf alone
 // is no number.
 __device__ __forceinline__ float inverse_of(float mo, float l) { return l != 0.f ? 1.0f / l : mo == -INFINITY ? 0.f : NAN; }

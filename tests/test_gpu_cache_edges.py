@@ -367,3 +367,23 @@ def test_answering_from_a_translated_context(which, dst_layout, page_layout):
             want, mag, smax = ref.paged_attention(flat, _np(k[l]), _np(v[l]), table.cpu().numpy(), [kv] * B, flat, max_new=n,
                                                   layout=page_layout)
             assert (np.abs(_np(o[l]).reshape(want.shape) - want) <= _bound(t, want, mag, smax, D, kv)).all(), (n, l)
+
+
+@pytest.mark.parametrize("t,n,G,D", [("bf16", 1, 6, 128), ("bf16", 3, 4, 64), ("bf16", 40, 4, 128), ("f32", 9, 2, 64), ("f32", 1, 2, 128)])
+def test_holes_in_cut_contexts(t, n, G, D):
+    """Long contexts that are holes throughout, or but for a page, or but for the last position's: rows that see
+    nothing are zeros, also where a window leaves them only holes."""
+    import torch
+    print("case cut holes", t, n, D, flush=True)
+    rng = np.random.default_rng(n + G)
+    c = Cache(rng, [3000, 2100, 1500, 70], 16, 2, D, t, max_pages=1024)
+    c.table[0] = -1
+    c.table[1, :60] = c.n_pages
+    c.table[1, 61:] = -7
+    c.table[2, :93] = -1
+    c.d_table = _i32(c.table)
+    q, _ = _rand(rng, (4, n, 2 * G, D), t)
+    for window in (0, 64, 1200):
+        o = _attend(c, q, window=window)
+        assert (o[0] == 0).all() and (window != 64 or (o[1] == 0).all())
+        assert torch.isfinite(_attend(c, q, window=window, scratch=False)).all()
