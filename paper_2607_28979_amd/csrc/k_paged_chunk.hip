@@ -5,8 +5,8 @@
 // Bound: issue. A wave's chunk is 32 matrix products (1024 cycles of its SIMD's matrix unit)
 // and about 850 cycles of softmax on the vector unit, of which 512 are the exponentials;
 // two workgroups share a CU, and what overlaps is one's products with the other's softmax.
-// 2 x 2048 tokens of 28 heads, head size 128, over contexts of 8192: 429 us, 0.98 PFLOP/s (a
-// plain 8192^3 bf16 product reaches 1.21 here). What led there from 562: operands of both
+// 2 x 2048 tokens of 28 heads, head size 128, over contexts of 8192: 403 to 436 us by the card, 0.97
+// to 1.04 PFLOP/s (a plain 8192^3 bf16 product reaches 1.21). What led there from 562: operands of both
 // products read ahead (541), a base that rarely moves (509), V rows swizzled for the
 // transposed reads (501), neighbouring tiles on one XCD (469; 490 on the card of the next figures), wave
 // priority to the products (475), no lane waiting for its row's other lane (443), row sums
@@ -17,8 +17,9 @@
 // The probabilities are rounded to bf16 for the second product, and a row's sum takes them as
 // rounded, so that the weights add up to 1.  The error against 64 bits is 2.35e-3 of the result,
 // 1.66e-3 of which is the result's own rounding.  As two bf16 terms, a product each, they would
-// leave that alone, at 607 us instead of 413 (1000 tokens on 4000 positions 114 and 91, 6 x 37
-// on 4096 20.9 and 19.5): the products are what bounds this kernel.
+// leave that alone, at 607 us instead of 413 (560 instead of 405 with every step's exponentials
+// beside the products of the step before; 1000 tokens on 4000 positions 114 and 91, 6 x 37 on
+// 4096 20.9 and 19.5): the products are what bounds this kernel.
 #include "paged_attn_device.h"
 
 namespace mot {

@@ -7,17 +7,17 @@
 // during this one's softmax, V after its second product.
 //
 // Bound: memory where contexts are long (48 sequences of 205 to 8192 positions, 4 KV heads
-// of 128, 207 MB: 46 us, 4.5 TB/s where a copy reaches 5.2), latency where they are short
-// (one of 1100: 7 us, and 3 of joining its parts).  The work is shared out (cut) rather
+// of 128, 207 MB: 47 us, 4.4 TB/s where a copy reaches 5.2), latency where they are short
+// (one of 1100: 8 us, and 3 of joining its parts).  The work is shared out (cut) rather
 // than a workgroup given to each sequence and KV head, since the longest sequence would
 // hold the call up: 104 us for the 48.  V read through the transposing LDS read with its own
-// wait: 63 -> 52 us.  Eight waves where there is a CU for every workgroup and nothing to
+// wait: 63 -> 52 us (with the join).  Eight waves where there is a CU for every workgroup and nothing to
 // cut, four else: eight leave room for one workgroup per CU only.
 //
 // The probabilities go into the second product as two bf16 terms, a product each: the matrix
-// unit is 5 % busy, and the error against 64 bits falls from 2.25e-3 to 1.66e-3 of the result,
+// unit is 7 % busy, and the error against 64 bits falls from 2.25e-3 to 1.66e-3 of the result,
 // which is the rounding of the result alone (the 48 sequences: 51.2 -> 52.2 us with the join,
-// one of 1100 10.4 -> 10.6).
+// one of 1100 10.4 -> 10.6; 48 of 2 heads of 64 19.7 -> 20.0).
 #include "paged_attn_device.h"
 
 namespace mot {

@@ -1,12 +1,15 @@
 // fp32 attention of new tokens over the paged cache (paged_attn_device.h says what a
 // workgroup computes): tiles of 16 query rows; the four waves take blocks of 32
 // positions in turn, each with its own tiles and no barrier, and are joined through LDS at
-// the end.  On v_mfma_f32_16x16x4_f32: exact fp32 products, a quarter of the rate that
-// the bf16 products reach with a sixteenth of the work per instruction.
+// the end.  On v_mfma_f32_16x16x4_f32: exact fp32 products, at a sixteenth of the rate of the
+// bf16 ones (as many cycles for a sixteenth of the work).
 //
 // Bound: latency for short contexts (3 x 64 tokens of 12 heads of 64 over 333 positions:
-// 9.5 us; tiles of 32 rows gave it too few workgroups, 24.7 us), issue of the fp32 products
-// for long ones (500 tokens of 12 heads of 128 over 2000: 96 us, 56 TFLOP/s).
+// 9.5 us; tiles of 32 rows gave it too few workgroups, 24.7 us).  Long ones reach 40 to 55 %
+// of a large product's rate (500 tokens of 12 heads of 128 over 2000: 98 us, 55 TFLOP/s; 1024
+// over 4096 301 us, 75): at D = 128 the 131 KB of LDS leave one workgroup to a CU and one wave to a
+// SIMD, whose products, softmax and masks follow one another, and K and V come again for
+// every 16 rows.
 #include "paged_attn_device.h"
 
 namespace mot {

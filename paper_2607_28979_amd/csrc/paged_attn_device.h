@@ -421,7 +421,7 @@ inline int64_t own_tiles(const AttendProblem& p, int rows) {
 // where it is cut; where decoding has several tiles to a sequence; and where packed tokens of
 // which one sequence might have most, but has not, would make most of own_work()'s grid leave
 // at once.  47 single tokens and 512 of one sequence, contexts of 1000, 28 heads on 4 of 128:
-// 96 and 36 us; 200 and 1500 on 1500: 316 and 169; fp32, 47 and 100 on 1000: 81 and 42.
+// 96 and 35 us; 200 and 1500 on 1500: 316 and 172; fp32, 47 and 100 on 1000: 81 and 33.
 inline bool finds_work(const AttendProblem& p, int rows) {
     const int64_t tiles = own_tiles(p, rows);
     if (p.part || rows == 32) return p.part || tiles > p.c.H_kv;
